@@ -398,6 +398,125 @@ int32_t co3_user_encode(const float *g, float *err, int64_t n, int32_t U, int64_
  */
 void co3_set_exchange_spin_limit(int64_t polls);
 
+/* ---- the server's update of the model ------------------------------------- */
+
+/*
+ * What follows the average of Algorithm 1 (the PS update): the global norm of a gradient that lies in many tensors,
+ * and the AdamW step on all of them in one launch, with states in 32 bits or in 8.
+ *
+ * Step t, every operation on its own rounded to fp32, scalars computed in fp64 and rounded once:
+ *     g' = factor * g;   m' = beta1 m + (1 - beta1) g';   v' = beta2 v + (1 - beta2) (g' g')
+ *     p' = p - ((lr_s weight_decay) p + (lr_s / (1 - beta1^t)) (m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)))
+ * with lr_s = lr * lr_scale of the tensor (sqrt and the quotient are correctly rounded).  Parameters and gradients are
+ * fp32, bf16 or fp16; a 16-bit parameter is rounded to nearest, ties to even, from the fp32 result, and the step starts
+ * from it, or, where a master array is given, from the fp32 value kept there (the parameter is then written only).
+ *
+ * Places.  The tensors of a call lie one behind another in the state arrays (moments, masters), in the order of the
+ * table: packed for 32-bit states, each begun at a multiple of 256 places for 8-bit ones.  co3_step_layout_of says how
+ * long the arrays are; places between the tensors are neither read into a result nor changed.
+ *
+ * 8-bit states.  Blocks of 256 places share a scale.  m and r = sqrt(v) are e4m3 numbers (1 sign, 4 exponent, 3 mantissa
+ * bits, exponent bias 7, gradual underflow, up to 448) under a scale of 8 bits s that stands for 2^(s - 127): the
+ * smallest one under which the block's largest magnitude stays within 448 however it is rounded.  The part
+ * that is cut off rounds the number up with its own probability: by 16 bits of a hash of (seed, t, place), the
+ * complement of m's for r, so that equal calls give equal results.  (Rounding to nearest would hold r where it is: a
+ * step moves v by some 1 - beta2 of itself, the next number is 12 % away.)  An r that is not zero does not become zero.
+ * Where a gradient is not finite its block's states become infinite.
+ */
+#define CO3_F32 0
+#define CO3_BF16 1
+#define CO3_F16 2
+#define CO3_NONE (-1)            /* param_type of a table for a norm alone */
+#define CO3_STEP_BLOCK 256       /* places that share a scale */
+#define CO3_STEP_CHUNK_BYTES 40  /* one entry of the plan */
+#define CO3_STEP_MAX_ELEMS ((int64_t)1 << 33)
+
+/* One tensor, contiguous; addresses are multiples of the element size (no more is asked of them). */
+typedef struct {
+    void *param;            /* device, n elements of param_type; NULL in a table for a norm alone */
+    const void *grad;       /* device, n elements of grad_type */
+    int64_t n;              /* elements, 0 allowed */
+    float lr_scale;         /* factor of the learning rate for this tensor */
+    float weight_decay;
+} co3_step_tensor;
+
+/* Sizes that follow from a table of tensors (a value of the host, filled by co3_step_layout_of). */
+typedef struct {
+    int64_t elems;          /* length of the state arrays (and of the master array), in elements */
+    int64_t blocks;         /* scales of each 8-bit state, 0 with 32-bit states */
+    int64_t chunks;         /* entries of the plan */
+    int64_t plan_bytes;     /* bytes of the plan, at least 16 */
+    int64_t partials;       /* partial sums (double) that a norm needs, at least 1 */
+    int32_t param_type, grad_type;
+    int32_t state_bits;     /* 32, 8, or 0 for a norm alone */
+    int32_t chunk;          /* elements of a tensor that one workgroup takes */
+} co3_step_layout;
+
+typedef struct {
+    double lr, beta1, beta2, eps; /* lr >= 0, 0 <= beta < 1, eps > 0 also in fp32 */
+    double grad_scale;            /* multiplies every gradient, > 0 (1: as they are) */
+    double max_norm;              /* > 0; the norm beyond which gradients are scaled down (INFINITY: never) */
+    int64_t t;                    /* number of this step, from 1; used where no co3_step_state is given */
+    uint64_t seed;                /* of the rounding of 8-bit states */
+} co3_adamw_args;
+
+/* Device memory of the caller, 8-byte aligned, zeroed once: what a step that the device counts goes by.  t is the number of steps
+ * taken, skipped how many were left out; norm and factor are those of the last co3_step_begin.  The rest is the
+ * library's. */
+typedef struct {
+    int64_t t, skipped;
+    float norm, factor;
+    int32_t reserved[10];
+} co3_step_state;
+
+/* Sizes for T >= 1 tensors.  Host only.  CO3_EINVAL: a null or misaligned address, a negative or too large size (elems
+ * <= 2^33), a factor that is negative or not finite, types or state_bits other than the above. */
+int32_t co3_step_layout_of(const co3_step_tensor *tensors_host, int32_t T, int32_t param_type, int32_t grad_type,
+                           int32_t state_bits, co3_step_layout *layout_host);
+
+/* The plan of a table: the tensors cut into chunks.  Host only; the caller copies the plan_bytes bytes to the device
+ * (8-byte aligned) and makes a new plan when a tensor moves or a factor changes.  CO3_EINVAL also where the layout is not
+ * this table's and where a parameter overlaps another one or a gradient. */
+int32_t co3_step_plan(const co3_step_tensor *tensors_host, int32_t T, const co3_step_layout *layout_host, void *plan_host,
+                      size_t plan_bytes);
+
+/* partials[layout->partials] = sums of squares, in fp64, of the gradients of a plan (one launch).  Several tables, as of
+ * models with parameters of several types, write one behind another and are finished together. */
+int32_t co3_grad_sumsq(const co3_step_layout *layout_host, const void *plan, double *partials, void *stream);
+
+/*
+ * Global norm of the gradients of a plan, and the factor that clips it:
+ *     out[0] = norm = grad_scale * sqrt(sum g^2),   out[1] = grad_scale * min(1, max_norm / (norm + 1e-6))
+ * out[1] is -1 where the sum is not finite.  partials: layout->partials doubles of workspace.  The sums are taken in a
+ * fixed order: equal calls give equal results.
+ */
+int32_t co3_grad_norm(const co3_step_layout *layout_host, const void *plan, double grad_scale, double max_norm, float *out,
+                      double *partials, void *stream);
+
+/*
+ * Begins a step that the device counts (for captured steps, clipped ones, learning rates that the device holds).
+ * partials: NULL (no norm is taken, the factor is grad_scale), or count sums of co3_grad_sumsq, from which norm and factor
+ * follow as in co3_grad_norm.  If the norm is not finite, state->skipped goes up, and the step that follows changes
+ * nothing; else state->t goes up.  lr_dev: NULL, or a device float that stands for args->lr.
+ */
+int32_t co3_step_begin(const co3_adamw_args *args_host, const double *partials, int64_t count, const float *lr_dev,
+                       co3_step_state *state, void *stream);
+
+/*
+ * AdamW on all tensors of a plan, with 32-bit (co3_adamw) or 8-bit states (co3_adamw8): one launch.
+ *   master   NULL, or [elems] f32 in/out for 16-bit parameters
+ *   m, v     [elems] f32 in/out, 4-byte aligned
+ *   m, r     [elems] e4m3 in/out, 4-byte aligned;  m_scale, r_scale [blocks] u8 in/out;  all zero at the start
+ *   state    NULL: the step is number args->t and the factor args->grad_scale; else what the last co3_step_begin on
+ *            this stream with the same args has left there
+ * Arrays are the caller's and must not overlap.  CO3_EINVAL for bad arguments, a layout of the other state_bits, masters
+ * of fp32 parameters.
+ */
+int32_t co3_adamw(const co3_step_layout *layout_host, const void *plan, float *master, float *m, float *v,
+                  const co3_adamw_args *args_host, const co3_step_state *state, void *stream);
+int32_t co3_adamw8(const co3_step_layout *layout_host, const void *plan, float *master, uint8_t *m, uint8_t *m_scale, uint8_t *r,
+                   uint8_t *r_scale, const co3_adamw_args *args_host, const co3_step_state *state, void *stream);
+
 /* ---- launch timing (diagnostic) ------------------------------------------ */
 
 /*
@@ -405,14 +524,14 @@ void co3_set_exchange_spin_limit(int64_t polls);
  * that must report one kernel's average duration.  Process-global and not thread-safe: the
  * only state the library keeps, and only while enabled.  kernel ids: 0 k_fill_i32, 1 k_absmax,
  * 2 k_convert_ef, 3 k_histogram, 4 k_build_code, 5 k_enc_sizes, 6 k_enc_scan, 7 k_enc_pack,
- * 8 k_decode, 9 k_ps_sum, 10 k_moments, 11 k_bias_scale, 12 k_coop_convert (co3_kernel_name returns
- * these names, "" for other ids).
+ * 8 k_decode, 9 k_ps_sum, 10 k_moments, 11 k_bias_scale, 12 k_coop_convert, 13 k_grad_sumsq,
+ * 14 k_step_begin, 15 k_adamw, 16 k_adamw8 (co3_kernel_name returns these names, "" for other ids).
  *   co3_timing_enable(mask): bracket every later launch of kernel k with events iff bit k is set.
  *   co3_timing_read(k, &ms, &count): waits for the recorded events, then returns the summed
  *       duration and launch count of kernel k since the last reset.
  *   co3_timing_reset(): waits likewise and clears all sums.
  */
-#define CO3_KERNEL_COUNT 13
+#define CO3_KERNEL_COUNT 17
 int32_t co3_timing_enable(uint32_t kernel_mask);
 int32_t co3_timing_read(int32_t kernel, double *total_ms, int64_t *launches);
 int32_t co3_timing_reset(void);

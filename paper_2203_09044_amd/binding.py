@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from typing import Optional
 
 import torch
 
@@ -30,12 +31,35 @@ EXPORTS = (
     "co3_convert_encode_workspace_bytes", "co3_convert_encode", "co3_convert_encode_layers", "co3_encode_static",
     "co3_user_encode_workspace_bytes", "co3_user_encode", "co3_set_exchange_spin_limit", "co3_design_layer_tables",
     "co3_ps_aggregate_partial", "co3_ps_decode_users", "co3_ps_average",
+    "co3_step_layout_of", "co3_step_plan", "co3_grad_sumsq", "co3_grad_norm", "co3_step_begin", "co3_adamw", "co3_adamw8",
 )
-KERNEL_COUNT = 13
+KERNEL_COUNT = 17
+TYPE_OF = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # CO3_F32, CO3_BF16, CO3_F16
+TYPE_NONE = -1
+STEP_BLOCK = 256
+STEP_STATE_BYTES = 64
 
 
 class _Fmt(C.Structure):
     _fields_ = [("exp_bits", C.c_int32), ("mant_bits", C.c_int32)]
+
+
+class StepTensor(C.Structure):
+    """One tensor of a table: addresses, size, its factors (co3_step_tensor)."""
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("n", C.c_int64), ("lr_scale", C.c_float), ("weight_decay", C.c_float)]
+
+
+class StepLayout(C.Structure):
+    """Sizes that follow from a table of tensors (co3_step_layout)."""
+    _fields_ = [("elems", C.c_int64), ("blocks", C.c_int64), ("chunks", C.c_int64), ("plan_bytes", C.c_int64),
+                ("partials", C.c_int64), ("param_type", C.c_int32), ("grad_type", C.c_int32), ("state_bits", C.c_int32),
+                ("chunk", C.c_int32)]
+
+
+class AdamwArgs(C.Structure):
+    """Scalars of a step (co3_adamw_args)."""
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("grad_scale", C.c_double), ("max_norm", C.c_double), ("t", C.c_int64), ("seed", C.c_uint64)]
 
 
 @dataclass(frozen=True)
@@ -128,6 +152,21 @@ def _load():
     L.co3_convert_encode_layers.restype = i32
     L.co3_convert_encode_layers.argtypes = [p, p, i64, i32, i64, p, i32, p, i32, p, C.c_float, _Fmt, p, p, i32, p, p, i64, i32,
                                             p, p, p, sz, p, p]
+    lay, arg = C.POINTER(StepLayout), C.POINTER(AdamwArgs)
+    L.co3_step_layout_of.restype = i32
+    L.co3_step_layout_of.argtypes = [C.POINTER(StepTensor), i32, i32, i32, i32, lay]
+    L.co3_step_plan.restype = i32
+    L.co3_step_plan.argtypes = [C.POINTER(StepTensor), i32, lay, p, sz]
+    L.co3_grad_sumsq.restype = i32
+    L.co3_grad_sumsq.argtypes = [lay, p, p, p]
+    L.co3_grad_norm.restype = i32
+    L.co3_grad_norm.argtypes = [lay, p, C.c_double, C.c_double, p, p, p]
+    L.co3_step_begin.restype = i32
+    L.co3_step_begin.argtypes = [arg, p, i64, p, p, p]
+    L.co3_adamw.restype = i32
+    L.co3_adamw.argtypes = [lay, p, p, p, p, arg, p, p]
+    L.co3_adamw8.restype = i32
+    L.co3_adamw8.argtypes = [lay, p, p, p, p, p, p, arg, p, p]
     L.co3_model_weights.restype = i32
     L.co3_model_weights.argtypes = [i32, _Fmt, C.c_double, C.c_double, p]
     L.co3_timing_enable.restype = i32
@@ -465,3 +504,67 @@ def ps_aggregate_layers(words, chunk_bitoff, chunk_syms, codes, code_seg_off, fm
                                       workspace.numel() * workspace.element_size(), _dp(status, torch.int32),
                                       _stream(stream))
     _chk(rc, "co3_ps_aggregate_layers")
+
+
+# ---- the server's update: gradient norm, AdamW over many tensors ------------------------------
+def step_layout_of(tensors, param_type: int, grad_type: int, state_bits: int) -> StepLayout:
+    """tensors: ctypes array of StepTensor (host computation)."""
+    out = StepLayout()
+    _chk(_lib.co3_step_layout_of(tensors, len(tensors), param_type, grad_type, state_bits, C.byref(out)), "co3_step_layout_of")
+    return out
+
+
+def step_plan(tensors, layout: StepLayout):
+    """Host computation; returns the plan as a CPU uint8 tensor, to be copied to the device."""
+    plan = torch.zeros((layout.plan_bytes // 8,), dtype=torch.int64)
+    _chk(_lib.co3_step_plan(tensors, len(tensors), C.byref(layout), C.c_void_p(plan.data_ptr()), layout.plan_bytes), "co3_step_plan")
+    return plan.view(torch.uint8)
+
+
+def _need(t, count: int, what: str):
+    if t.numel() < count:
+        raise ValueError(f"{what}: {count} elements are needed, got {t.numel()}")
+
+
+def _step_arrays(layout: StepLayout, plan, **arrays):
+    _need(plan, layout.plan_bytes, "plan")
+    for name, (t, count) in arrays.items():
+        if t is not None:
+            _need(t, count, name)
+
+
+def grad_sumsq(layout: StepLayout, plan, partials, stream=None):
+    _step_arrays(layout, plan, partials=(partials, layout.partials))
+    _chk(_lib.co3_grad_sumsq(C.byref(layout), _dp(plan, torch.uint8), _dp(partials, torch.float64), _stream(stream)), "co3_grad_sumsq")
+
+
+def grad_norm(layout: StepLayout, plan, grad_scale: float, max_norm: float, out, partials, stream=None):
+    """out: 2 float32 on the device (norm, factor); partials: float64 workspace."""
+    _step_arrays(layout, plan, partials=(partials, layout.partials), out=(out, 2))
+    _chk(_lib.co3_grad_norm(C.byref(layout), _dp(plan, torch.uint8), grad_scale, max_norm, _dp(out, torch.float32),
+                            _dp(partials, torch.float64), _stream(stream)), "co3_grad_norm")
+
+
+def step_begin(args: AdamwArgs, state, partials=None, count: Optional[int] = None, lr=None, stream=None):
+    """state: 64 bytes (uint8) on the device; partials: None, or the sums of co3_grad_sumsq; lr: None, or one float32."""
+    _need(state, STEP_STATE_BYTES, "state")
+    if partials is not None and (partials.numel() if count is None else count) > partials.numel():
+        raise ValueError("count is more than there are partial sums")
+    n = 0 if partials is None else partials.numel() if count is None else count
+    _chk(_lib.co3_step_begin(C.byref(args), _dp(partials, torch.float64), n, _dp(lr, torch.float32), _dp(state, torch.uint8),
+                             _stream(stream)), "co3_step_begin")
+
+
+def adamw(layout: StepLayout, plan, m, v, args: AdamwArgs, state=None, master=None, stream=None):
+    _step_arrays(layout, plan, m=(m, layout.elems), v=(v, layout.elems), master=(master, layout.elems), state=(state, STEP_STATE_BYTES))
+    _chk(_lib.co3_adamw(C.byref(layout), _dp(plan, torch.uint8), _dp(master, torch.float32), _dp(m, torch.float32),
+                        _dp(v, torch.float32), C.byref(args), _dp(state, torch.uint8), _stream(stream)), "co3_adamw")
+
+
+def adamw8(layout: StepLayout, plan, m, m_scale, r, r_scale, args: AdamwArgs, state=None, master=None, stream=None):
+    """m, r: float8_e4m3fn; m_scale, r_scale: float8_e8m0fnu (their bytes as the C entry takes them)."""
+    _step_arrays(layout, plan, m=(m, layout.elems), r=(r, layout.elems), m_scale=(m_scale, layout.blocks),
+                 r_scale=(r_scale, layout.blocks), master=(master, layout.elems), state=(state, STEP_STATE_BYTES))
+    e, s = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    _chk(_lib.co3_adamw8(C.byref(layout), _dp(plan, torch.uint8), _dp(master, torch.float32), _dp(m, e), _dp(m_scale, s), _dp(r, e),
+                         _dp(r_scale, s), C.byref(args), _dp(state, torch.uint8), _stream(stream)), "co3_adamw8")

@@ -3,7 +3,9 @@
 
 #include "co3_dev.h"
 #include "kernels.h"
+#include "step.h"
 
+#include <algorithm>
 #include <atomic>
 #include <vector>
 
@@ -130,7 +132,8 @@ const char *co3_kernel_name(int32_t kernel)
 {
     static const char *names[CO3_K_COUNT] = {"k_fill_i32", "k_absmax",    "k_convert_ef", "k_histogram", "k_build_code",
                                              "k_enc_sizes", "k_enc_scan", "k_enc_pack",   "k_decode",    "k_ps_sum",
-                                             "k_moments",  "k_bias_scale", "k_coop_convert"};
+                                             "k_moments",  "k_bias_scale", "k_coop_convert", "k_grad_sumsq", "k_step_begin",
+                                             "k_adamw",    "k_adamw8"};
     return (kernel >= 0 && kernel < CO3_K_COUNT) ? names[kernel] : "";
 }
 
@@ -601,6 +604,195 @@ int32_t co3_ps_aggregate_layers(const uint64_t *words, int64_t cap_words, const 
     if (!code_seg_off) return CO3_EINVAL;
     return aggregate_common(words, cap_words, chunk_bitoff, chunk_syms, codes, code_seg_off, code_nseg, fmt, n, U,
                             anchor, scale, seg_off, nseg, avg_out, workspace, ws_bytes, status, stream);
+}
+
+// ---- the server's update --------------------------------------------------------------------
+
+static size_t type_bytes(int32_t type) { return type == CO3_F32 ? 4 : 2; }
+
+static bool type_ok(int32_t type) { return type == CO3_F32 || type == CO3_BF16 || type == CO3_F16; }
+
+// not negative and finite
+static bool factor_ok(double x) { return x >= 0.0 && x - x == 0.0; }
+
+// Elements of a tensor that one workgroup takes.  A workgroup of 256 lanes with four elements each has 1024 in
+// flight; one such piece per workgroup spreads a small model over the most compute units, longer ones save
+// table entries and starts.
+static int32_t step_chunk(int64_t total) { return total <= ((int64_t)1 << 22) ? 1024 : 4096; }
+
+#define CO3_STEP_PARTIALS_MAX 1024
+
+int32_t co3_step_layout_of(const co3_step_tensor *tensors, int32_t T, int32_t param_type, int32_t grad_type, int32_t state_bits,
+                           co3_step_layout *out)
+{
+    if (!tensors || !out || T < 1 || !type_ok(grad_type)) return CO3_EINVAL;
+    if (state_bits != 0 && state_bits != 8 && state_bits != 32) return CO3_EINVAL;
+    if (state_bits == 0 ? param_type != CO3_NONE : !type_ok(param_type)) return CO3_EINVAL;
+    const int64_t unit = state_bits == 8 ? CO3_STEP_BLOCK : 1;
+    int64_t total = 0, elems = 0;
+    for (int32_t k = 0; k < T; ++k) {
+        const co3_step_tensor &x = tensors[k];
+        if (x.n < 0 || x.n > CO3_STEP_MAX_ELEMS || !factor_ok(x.lr_scale) || !factor_ok(x.weight_decay)) return CO3_EINVAL;
+        if (x.n > 0 && (!x.grad || !aligned(x.grad, type_bytes(grad_type)))) return CO3_EINVAL;
+        if (x.n > 0 && state_bits != 0 && (!x.param || !aligned(x.param, type_bytes(param_type)))) return CO3_EINVAL;
+        total += x.n;
+        elems += (x.n + unit - 1) / unit * unit;
+        if (elems > CO3_STEP_MAX_ELEMS) return CO3_EINVAL;
+    }
+    const int32_t chunk = step_chunk(total);
+    int64_t chunks = 0;
+    for (int32_t k = 0; k < T; ++k) chunks += (tensors[k].n + chunk - 1) / chunk;
+    *out = co3_step_layout{};
+    out->elems = elems;
+    out->blocks = state_bits == 8 ? elems / CO3_STEP_BLOCK : 0;
+    out->chunks = chunks;
+    out->plan_bytes = chunks > 0 ? chunks * CO3_STEP_CHUNK_BYTES : 16;
+    out->partials = chunks < 1 ? 1 : chunks < CO3_STEP_PARTIALS_MAX ? chunks : CO3_STEP_PARTIALS_MAX;
+    out->param_type = param_type;
+    out->grad_type = grad_type;
+    out->state_bits = state_bits;
+    out->chunk = chunk;
+    return CO3_OK;
+}
+
+// whether a parameter shares memory with another one or with a gradient (gradients are only read)
+static bool params_overlap(const co3_step_tensor *tensors, int32_t T, size_t param_bytes, size_t grad_bytes)
+{
+    struct Span {
+        uintptr_t lo, hi;
+        bool param;
+    };
+    std::vector<Span> spans;
+    spans.reserve(2 * (size_t)T);
+    for (int32_t k = 0; k < T; ++k) {
+        const co3_step_tensor &x = tensors[k];
+        if (x.n == 0) continue;
+        const uintptr_t p = reinterpret_cast<uintptr_t>(x.param), g = reinterpret_cast<uintptr_t>(x.grad);
+        spans.push_back({p, p + (uintptr_t)x.n * param_bytes, true});
+        spans.push_back({g, g + (uintptr_t)x.n * grad_bytes, false});
+    }
+    std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.lo < b.lo; });
+    uintptr_t end_any = 0, end_param = 0;        // furthest end so far of any span, of a parameter's
+    for (const Span &s : spans) {
+        if (s.lo < end_param || (s.param && s.lo < end_any)) return true;
+        end_any = std::max(end_any, s.hi);
+        if (s.param) end_param = std::max(end_param, s.hi);
+    }
+    return false;
+}
+
+int32_t co3_step_plan(const co3_step_tensor *tensors, int32_t T, const co3_step_layout *layout, void *plan_host, size_t plan_bytes)
+{
+    if (!layout || !plan_host || !aligned(plan_host, 8)) return CO3_EINVAL;
+    co3_step_layout own;
+    const int32_t rc = co3_step_layout_of(tensors, T, layout->param_type, layout->grad_type, layout->state_bits, &own);
+    if (rc != CO3_OK) return rc;
+    if (own.elems != layout->elems || own.blocks != layout->blocks || own.chunks != layout->chunks || own.chunk != layout->chunk ||
+        own.plan_bytes != layout->plan_bytes || own.partials != layout->partials || plan_bytes < (size_t)own.plan_bytes)
+        return CO3_EINVAL;
+    const size_t pb = own.state_bits ? type_bytes(own.param_type) : 0, gb = type_bytes(own.grad_type);
+    if (own.state_bits) {
+        try {
+            if (params_overlap(tensors, T, pb, gb)) return CO3_EINVAL;
+        } catch (...) {                          // no memory for the check
+            return CO3_EINVAL;
+        }
+    }
+    const int64_t unit = own.state_bits == 8 ? CO3_STEP_BLOCK : 1;
+    Co3StepChunk *c = static_cast<Co3StepChunk *>(plan_host);
+    int64_t place = 0;
+    for (int32_t k = 0; k < T; ++k) {
+        const co3_step_tensor &x = tensors[k];
+        for (int64_t i = 0; i < x.n; i += own.chunk, ++c) {
+            c->param = pb ? static_cast<char *>(x.param) + (size_t)i * pb : nullptr;
+            c->grad = static_cast<const char *>(x.grad) + (size_t)i * gb;
+            c->state = place + i;
+            c->count = (int32_t)std::min<int64_t>(own.chunk, x.n - i);
+            c->lr_scale = x.lr_scale;
+            c->weight_decay = x.weight_decay;
+            c->reserved = 0;
+        }
+        place += (x.n + unit - 1) / unit * unit;
+    }
+    return CO3_OK;
+}
+
+static bool layout_ok(const co3_step_layout *L, const void *plan)
+{
+    return L && plan && aligned(plan, 8) && L->chunks >= 0 && L->chunks <= CO3_STEP_MAX_ELEMS && L->elems >= 0 &&
+           L->elems <= CO3_STEP_MAX_ELEMS && L->partials >= 1 && L->partials <= CO3_STEP_PARTIALS_MAX && type_ok(L->grad_type) &&
+           (L->state_bits == 0 || ((L->state_bits == 8 || L->state_bits == 32) && type_ok(L->param_type)));
+}
+
+static bool norm_args_ok(double grad_scale, double max_norm)
+{
+    return grad_scale > 0.0 && factor_ok(grad_scale) && max_norm > 0.0;
+}
+
+static bool adamw_args_ok(const co3_adamw_args *a)
+{
+    return a && factor_ok(a->lr) && a->beta1 >= 0.0 && a->beta1 < 1.0 && a->beta2 >= 0.0 && a->beta2 < 1.0 && factor_ok(a->eps) &&
+           (float)a->eps > 0.0f && norm_args_ok(a->grad_scale, a->max_norm);
+}
+
+int32_t co3_grad_sumsq(const co3_step_layout *layout, const void *plan, double *partials, void *stream)
+{
+    if (!layout_ok(layout, plan) || !partials || !aligned(partials, 8)) return CO3_EINVAL;
+    return hip_rc(co3_launch_grad_sumsq(layout, plan, partials, static_cast<hipStream_t>(stream)));
+}
+
+int32_t co3_grad_norm(const co3_step_layout *layout, const void *plan, double grad_scale, double max_norm, float *out,
+                      double *partials, void *stream)
+{
+    if (!out || !aligned(out, 4) || !norm_args_ok(grad_scale, max_norm)) return CO3_EINVAL;
+    const int32_t rc = co3_grad_sumsq(layout, plan, partials, stream);
+    if (rc != CO3_OK) return rc;
+    return hip_rc(co3_launch_norm_finish(partials, layout->chunks ? layout->partials : 0, grad_scale, max_norm, out,
+                                         static_cast<hipStream_t>(stream)));
+}
+
+int32_t co3_step_begin(const co3_adamw_args *args, const double *partials, int64_t count, const float *lr_dev,
+                       co3_step_state *state, void *stream)
+{
+    if (!adamw_args_ok(args) || !state || !aligned(state, 8) || count < 0 || (partials && !aligned(partials, 8))) return CO3_EINVAL;
+    if (lr_dev && !aligned(lr_dev, 4)) return CO3_EINVAL;
+    return hip_rc(co3_launch_step_begin(partials, count, args, lr_dev, state, static_cast<hipStream_t>(stream)));
+}
+
+static int32_t adamw_common(const co3_step_layout *layout, const void *plan, int32_t state_bits, float *master, void *m,
+                            uint8_t *m_scale, void *v, uint8_t *v_scale, const co3_adamw_args *args, const co3_step_state *state,
+                            void *stream)
+{
+    if (!layout_ok(layout, plan) || layout->state_bits != state_bits || !adamw_args_ok(args)) return CO3_EINVAL;
+    if (!m || !v || !aligned(m, 4) || !aligned(v, 4) || (state_bits == 8 && (!m_scale || !v_scale))) return CO3_EINVAL;
+    if (master && (layout->param_type == CO3_F32 || !aligned(master, 4))) return CO3_EINVAL;
+    if (!state && args->t < 1) return CO3_EINVAL;
+    if (state && !aligned(state, 8)) return CO3_EINVAL;
+    Co3StepLaunch s{};
+    s.layout = layout;
+    s.plan = plan;
+    s.master = master;
+    s.m = m;
+    s.v = v;
+    s.m_scale = m_scale;
+    s.v_scale = v_scale;
+    s.fix = {(float)args->beta1, (float)(1.0 - args->beta1), (float)args->beta2, (float)(1.0 - args->beta2), (float)args->eps};
+    s.factor = (float)args->grad_scale;
+    if (!state) s.var = co3_step_var(*args);
+    s.state = state;
+    return hip_rc(co3_launch_adamw(s, static_cast<hipStream_t>(stream)));
+}
+
+int32_t co3_adamw(const co3_step_layout *layout, const void *plan, float *master, float *m, float *v, const co3_adamw_args *args,
+                  const co3_step_state *state, void *stream)
+{
+    return adamw_common(layout, plan, 32, master, m, nullptr, v, nullptr, args, state, stream);
+}
+
+int32_t co3_adamw8(const co3_step_layout *layout, const void *plan, float *master, uint8_t *m, uint8_t *m_scale, uint8_t *r,
+                   uint8_t *r_scale, const co3_adamw_args *args, const co3_step_state *state, void *stream)
+{
+    return adamw_common(layout, plan, 8, master, m, m_scale, r, r_scale, args, state, stream);
 }
 
 // ---- model table (host arithmetic only) ---------------------------------------------------

@@ -8,7 +8,8 @@
 // Kernel ids for the optional launch timing (co3_timing_* in the public header).
 enum Co3Kernel {
     CO3_K_FILL = 0, CO3_K_ABSMAX, CO3_K_CONVERT, CO3_K_HISTOGRAM, CO3_K_BUILD, CO3_K_ENC_SIZES, CO3_K_ENC_SCAN,
-    CO3_K_ENC_PACK, CO3_K_DECODE, CO3_K_PS_SUM, CO3_K_MOMENTS, CO3_K_BIAS_SCALE, CO3_K_COOP, CO3_K_COUNT
+    CO3_K_ENC_PACK, CO3_K_DECODE, CO3_K_PS_SUM, CO3_K_MOMENTS, CO3_K_BIAS_SCALE, CO3_K_COOP, CO3_K_GRAD_SUMSQ,
+    CO3_K_STEP_BEGIN, CO3_K_ADAMW, CO3_K_ADAMW8, CO3_K_COUNT
 };
 
 // Brackets one kernel launch with a pair of HIP events on the launch stream when timing of that

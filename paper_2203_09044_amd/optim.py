@@ -1,0 +1,319 @@
+"""The server's update of a model that lies in many tensors: the global norm of the gradient and the AdamW step, each one
+pass over all of them.
+
+The handles hold what the calls need on the device (the plan of the tensors' chunks, states, partial sums) and issue
+them; all arithmetic runs in the HIP kernels (``co3_grad_norm``, ``co3_adamw``, ``co3_adamw8``).  Calls are issued on the
+current stream of the tensors' device and return without waiting.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+from typing import List, Optional, Sequence, Union
+
+import torch
+
+from . import binding as B
+
+PerTensor = Union[float, Sequence[float]]
+
+
+def _per_tensor(x: PerTensor, T: int, what: str) -> List[float]:
+    values = [float(x)] * T if isinstance(x, (int, float)) else [float(v) for v in x]
+    if len(values) != T:
+        raise ValueError(f"{what}: one value per tensor is needed ({T}), got {len(values)}")
+    if not all(v >= 0.0 and math.isfinite(v) for v in values):
+        raise ValueError(f"{what} must be finite and not negative")
+    return values
+
+
+def _check_tensors(tensors: Sequence[torch.Tensor], what: str):
+    if not tensors:
+        raise ValueError(f"no {what}")
+    first = tensors[0]
+    for t in tensors:
+        if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+            raise ValueError(f"{what}: CUDA tensors are needed")
+        if t.dtype not in B.TYPE_OF or t.dtype != first.dtype:
+            raise ValueError(f"{what}: all of one type out of float32, bfloat16 and float16 (a handle per type where a model mixes them)")
+        if t.device != first.device:
+            raise ValueError(f"{what}: all on one device")
+        if not t.is_contiguous():
+            raise ValueError(f"{what}: contiguous tensors are needed")
+
+
+class _Table:
+    """Plan of a list of tensors on their device.  The addresses are looked at before every use, and a new plan is made when
+    a tensor has moved."""
+
+    def __init__(self, params: Optional[Sequence[torch.Tensor]], grads: Sequence[torch.Tensor], state_bits: int,
+                 lr_scales: PerTensor = 1.0, weight_decays: PerTensor = 0.0):
+        self.params = None if params is None else list(params)
+        if self.params is not None:
+            _check_tensors(self.params, "parameters")
+        self.state_bits = state_bits
+        self._take(grads)
+        T = len(self.grads)
+        self.device = self.grads[0].device
+        self.lr_scales, self.weight_decays = _per_tensor(lr_scales, T, "lr_scales"), _per_tensor(weight_decays, T, "weight_decay")
+        self._captured = []                      # plans that a captured graph goes on reading
+        self._make()
+
+    def _take(self, grads: Sequence[torch.Tensor]):
+        grads = list(grads)
+        _check_tensors(grads, "gradients")
+        like = self.params if self.params is not None else getattr(self, "grads", None)
+        if like is not None and (len(like) != len(grads) or any(p.numel() != g.numel() for p, g in zip(like, grads))):
+            raise ValueError("gradients: one per parameter, with as many elements")
+        if like is not None and grads[0].device != like[0].device:
+            raise ValueError("gradients: on the parameters' device")
+        self.grads = grads
+
+    def _addresses(self) -> List[int]:
+        a = [g.data_ptr() for g in self.grads]
+        return a if self.params is None else a + [p.data_ptr() for p in self.params]
+
+    def _make(self):
+        self._at = self._addresses()
+        T = len(self.grads)
+        rows = (B.StepTensor * T)()
+        for k, g in enumerate(self.grads):
+            rows[k] = B.StepTensor(None if self.params is None else self._at[T + k], self._at[k], g.numel(), self.lr_scales[k],
+                                   self.weight_decays[k])
+        self.layout = B.step_layout_of(rows, B.TYPE_NONE if self.params is None else B.TYPE_OF[self.params[0].dtype],
+                                       B.TYPE_OF[self.grads[0].dtype], self.state_bits)
+        self.layout_ref = C.byref(self.layout)
+        try:
+            host = B.step_plan(rows, self.layout)
+        except B.Co3Error as e:
+            raise ValueError("a parameter shares memory with another one or with a gradient") from e
+        with torch.cuda.device(self.device):
+            self.plan = host.to(self.device)
+            self._home = torch.cuda.current_stream(self.device).cuda_stream
+        self.plan_ptr = C.c_void_p(self.plan.data_ptr())
+
+    def ready(self, grads: Optional[Sequence[torch.Tensor]]) -> int:
+        """The plan is that of the tensors as they lie now; returns the raw current stream of their device."""
+        if grads is not None:
+            was = self.grads[0].dtype
+            self._take(grads)
+            if self.grads[0].dtype != was:
+                self._at = None
+        capturing = torch.cuda.is_current_stream_capturing()
+        if self._at != self._addresses():
+            if capturing:
+                raise RuntimeError("a tensor has moved since the last step: step once before the capture")
+            self._make()
+        stream = torch.cuda.current_stream(self.device)
+        raw = stream.cuda_stream
+        if capturing and not any(p is self.plan for p in self._captured):
+            self._captured.append(self.plan)
+        elif raw != self._home:
+            self.plan.record_stream(stream)
+        return raw
+
+
+class _OnDevice:
+    """Launches of a handle go to its tensors' device, whichever is current."""
+
+    def _guard(self):
+        return torch.cuda.device(self._table.device)
+
+
+class GradNorm(_OnDevice):
+    """Global L2 norm of gradients that lie in many tensors, with the factor that clips it.
+
+    ``compute()`` returns a float32 tensor of two on the device, (norm, factor): norm = grad_scale * sqrt(sum g^2),
+    factor = grad_scale * min(1, max_norm / (norm + 1e-6)), or -1 where the norm is not finite.  The tensor is the handle's: the
+    next call overwrites it."""
+
+    def __init__(self, grads: Sequence[torch.Tensor], max_norm: float = math.inf, grad_scale: float = 1.0):
+        if not max_norm > 0.0 or not (grad_scale > 0.0 and math.isfinite(grad_scale)):
+            raise ValueError("max_norm and grad_scale must be positive, grad_scale finite")
+        self.max_norm, self.grad_scale = float(max_norm), float(grad_scale)
+        self._table = _Table(None, grads, 0)
+        dev = self._table.device
+        self._out = torch.zeros(2, dtype=torch.float32, device=dev)
+        self._partials = torch.empty(self._table.layout.partials, dtype=torch.float64, device=dev)
+        self._ptrs = C.c_void_p(self._out.data_ptr()), C.c_void_p(self._partials.data_ptr())
+
+    def compute(self, grads: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
+        """``grads``: None, or tensors of the same sizes to take instead, from now on."""
+        t = self._table
+        with self._guard():
+            raw = t.ready(grads)
+            B._chk(B._lib.co3_grad_norm(t.layout_ref, t.plan_ptr, self.grad_scale, self.max_norm, self._ptrs[0], self._ptrs[1],
+                                        C.c_void_p(raw)), "co3_grad_norm")
+        return self._out
+
+
+class AdamW(_OnDevice):
+    """AdamW over many tensors at once (the formulas: ``include/co3.h``).
+
+    params, grads   tensors of one type each (float32, bfloat16, float16), contiguous, on one device; written and read in place
+    lr              a float, or a float32 tensor of one element on the device (read at every step, also of a replayed graph)
+    weight_decay, lr_scales   one value, or one per tensor
+    state_bits      32: ``m``, ``v`` float32.  8: ``m``, ``r`` float8_e4m3fn with ``m_scale``, ``r_scale`` float8_e8m0fnu per 256 elements
+                    (r = sqrt(v)), rounded at random by a hash of ``seed``, the step and the place
+    master          16-bit parameters: float32 values kept in ``master``, taken from the parameters at the start
+    max_norm        None, or the global norm beyond which the gradients are scaled down; a step whose norm is not finite changes
+                    nothing and does not count (``skipped``)
+    grad_scale      multiplies every gradient (1 / loss scale, say)
+    device_steps    the device counts the steps, which a captured step needs (always so with max_norm or a tensor ``lr``)
+
+    The state arrays hold the tensors one behind another: packed with 32 bits, each from a multiple of 256 on with 8.
+    """
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: Union[float, torch.Tensor] = 1e-3,
+                 betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: PerTensor = 0.01, lr_scales: PerTensor = 1.0,
+                 state_bits: int = 32, master: bool = False, max_norm: Optional[float] = None, grad_scale: float = 1.0, seed: int = 0,
+                 device_steps: bool = False):
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        if not all(0.0 <= b < 1.0 for b in betas):
+            raise ValueError("betas must be in [0, 1)")
+        if not (C.c_float(eps).value > 0.0 and math.isfinite(eps)):
+            raise ValueError("eps must be positive, in float32 too")
+        if max_norm is not None and not max_norm > 0.0:
+            raise ValueError("max_norm must be positive")
+        if not (grad_scale > 0.0 and math.isfinite(grad_scale)):
+            raise ValueError("grad_scale must be positive and finite")
+        self._table = t = _Table(params, grads, state_bits, lr_scales, weight_decay)
+        if master and t.params[0].dtype == torch.float32:
+            raise ValueError("float32 parameters are their own masters")
+        self.state_bits, self.max_norm = state_bits, max_norm
+        self._args = B.AdamwArgs(0.0, betas[0], betas[1], eps, grad_scale, math.inf if max_norm is None else max_norm, 0,
+                                 seed & 0xFFFFFFFFFFFFFFFF)
+        self._args_ref = C.byref(self._args)
+        z = dict(device=t.device)
+        n, blocks = t.layout.elems, t.layout.blocks
+        if state_bits == 32:
+            self.m, self.v = (torch.zeros(n, dtype=torch.float32, **z) for _ in range(2))
+            states = (self.m, self.v)
+        else:
+            self.m, self.r = (torch.zeros(n, dtype=torch.uint8, **z).view(torch.float8_e4m3fn) for _ in range(2))
+            self.m_scale, self.r_scale = (torch.zeros(blocks, dtype=torch.uint8, **z).view(torch.float8_e8m0fnu) for _ in range(2))
+            states = (self.m, self.m_scale, self.r, self.r_scale)
+        self.master = None
+        if master:
+            self.master = torch.zeros(n, dtype=torch.float32, **z)
+            self.take_masters()
+        # an array of no elements has no address: any will do, none is read
+        self._state_ptrs = [C.c_void_p(s.data_ptr() or t.plan.data_ptr()) for s in states]
+        self._master_ptr = None if self.master is None else C.c_void_p(self.master.data_ptr() or t.plan.data_ptr())
+        self._step_fn = B._lib.co3_adamw if state_bits == 32 else B._lib.co3_adamw8
+        self._t = 0
+        self._dev = torch.zeros(B.STEP_STATE_BYTES // 8, dtype=torch.int64, **z)
+        self._dev_ptr = C.c_void_p(self._dev.data_ptr())
+        self.norm = self._dev.view(torch.float32)[4:6]        # (norm, factor) of the last step that took a norm
+        self._partials = torch.empty(t.layout.partials if max_norm is not None else 1, dtype=torch.float64, **z)
+        self._device_steps = device_steps or max_norm is not None
+        self.lr = lr
+
+    # ---- what a program sets and reads
+    @property
+    def lr(self):
+        return self._lr
+
+    @lr.setter
+    def lr(self, lr):
+        if isinstance(lr, torch.Tensor):
+            if lr.dtype != torch.float32 or lr.numel() != 1 or lr.device != self._table.device:
+                raise ValueError("lr: a float32 tensor of one element on the parameters' device")
+            if not self._on_device:
+                self._dev[0] = self._t
+                self._device_steps = True
+            self._args.lr = 0.0
+        elif not (lr >= 0.0 and math.isfinite(lr)):
+            raise ValueError("lr must be finite and not negative")
+        else:
+            self._args.lr = float(lr)
+        self._lr = lr
+
+    @property
+    def _on_device(self) -> bool:
+        return self._device_steps
+
+    @property
+    def t(self) -> int:
+        """Number of steps taken (waits for the device where that counts them)."""
+        return int(self._dev[0].item()) if self._on_device else self._t
+
+    @t.setter
+    def t(self, t: int):
+        if t < 0:
+            raise ValueError("t must not be negative")
+        self._t = int(t)
+        self._dev[0] = int(t)
+
+    @property
+    def skipped(self) -> int:
+        """Steps left out because their norm was not finite (waits for the device)."""
+        return int(self._dev[1].item())
+
+    def _views(self, flat: torch.Tensor) -> List[torch.Tensor]:
+        unit, at, out = B.STEP_BLOCK if self.state_bits == 8 else 1, 0, []
+        for p in self._table.params:
+            out.append(flat[at:at + p.numel()].view(p.shape))
+            at += (p.numel() + unit - 1) // unit * unit
+        return out
+
+    def take_masters(self):
+        """Masters as the parameters are now (after the parameters were loaded from elsewhere)."""
+        if self.master is not None:
+            for w, p in zip(self._views(self.master), self._table.params):
+                w.copy_(p.detach())
+
+    def moments(self):
+        """(m, v) of every tensor as float32 copies, whatever the states are kept in."""
+        if self.state_bits == 32:
+            m, v = self.m.clone(), self.v.clone()
+        else:
+            wide = lambda x, s: (x.float().view(-1, B.STEP_BLOCK) * s.float()[:, None]).view(-1)  # noqa: E731
+            m, v = wide(self.m, self.m_scale), wide(self.r, self.r_scale).square()
+        return list(zip(self._views(m), self._views(v)))
+
+    def _named(self):
+        names = ("m", "v") if self.state_bits == 32 else ("m", "m_scale", "r", "r_scale")
+        out = {k: getattr(self, k) for k in names}
+        if self.master is not None:
+            out["master"] = self.master
+        return out
+
+    def state_dict(self) -> dict:
+        return {"t": self.t, "skipped": self.skipped, "seed": int(self._args.seed), **{k: v.clone() for k, v in self._named().items()}}
+
+    def load_state_dict(self, d: dict):
+        named = self._named()
+        for k, v in named.items():
+            if k not in d or d[k].dtype != v.dtype or d[k].shape != v.shape:
+                raise ValueError(f"state_dict: {k} is missing or of another type or size")
+        for k, v in named.items():
+            v.copy_(d[k])
+        self._args.seed = d["seed"]
+        self.t = d["t"]
+        self._dev[1] = d["skipped"]
+
+    # ---- the step
+    def step(self, grads: Optional[Sequence[torch.Tensor]] = None):
+        """One step on every tensor.  ``grads``: None, or tensors of the same sizes to take instead, from now on."""
+        t = self._table
+        with self._guard():
+            raw = t.ready(grads)
+            stream = C.c_void_p(raw)
+            state = None
+            if self._on_device:
+                state, partials, count = self._dev_ptr, None, 0
+                if self.max_norm is not None:
+                    partials, count = C.c_void_p(self._partials.data_ptr()), t.layout.partials if t.layout.chunks else 0
+                    B._chk(B._lib.co3_grad_sumsq(t.layout_ref, t.plan_ptr, partials, stream), "co3_grad_sumsq")
+                lr = C.c_void_p(self._lr.data_ptr()) if isinstance(self._lr, torch.Tensor) else None
+                B._chk(B._lib.co3_step_begin(self._args_ref, partials, count, lr, state, stream), "co3_step_begin")
+            else:
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("a captured step needs device_steps=True")
+                self._args.t = self._t + 1
+            B._chk(self._step_fn(t.layout_ref, t.plan_ptr, self._master_ptr, *self._state_ptrs, self._args_ref, state, stream),
+                   "co3_adamw" if self.state_bits == 32 else "co3_adamw8")
+            if state is None:
+                self._t += 1

@@ -24,6 +24,7 @@ from co3_inputs import group_small_tensors, seg_offsets
 
 from . import binding as B
 from .binding import Fmt
+from .optim import AdamW
 from .pipeline import Co3Pipeline
 
 
@@ -80,7 +81,7 @@ class Co3SGD:
         for u, (x, y) in enumerate(batches):
             self.g[u].zero_()
             for p, v in zip(self.params, self.grad_views[u]):
-                p.grad = v
+                p.grad = v if p.dtype == v.dtype else None       # gradients of 16-bit parameters are copied in below
             loss = loss_fn(self.model(x), y)
             loss.backward()
             total += float(loss.detach())
@@ -154,3 +155,30 @@ class Co3SGD:
 
     def bits_per_element(self) -> float:
         return float(self.pipe.total_bits.sum().item()) / (self.U * self.n)
+
+
+class Co3AdamW(Co3SGD):
+    """Algorithm 1 with AdamW as the parameter server's update: the averaged reconstruction steps all tensors of the model in
+    one pass, clipped by its global norm where ``max_norm`` is given, with states in 32 bits or in 8 (``optim.AdamW``).  Tensors of
+    one dimension (biases, scales of norms) are not decayed unless ``decay_vectors``.  16-bit models get 32-bit masters.  The
+    other arguments are those of ``Co3SGD``."""
+
+    def __init__(self, model: torch.nn.Module, users: int, fmt: Fmt, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: float = 0.01, state_bits: int = 32, max_norm: Optional[float] = None, seed: int = 0,
+                 decay_vectors: bool = False, **codec):
+        super().__init__(model, users, fmt, lr, **codec)
+        self._stepped = self.pipe.avg                     # the average whose segments the optimiser holds
+        decays = [weight_decay if decay_vectors or p.dim() > 1 else 0.0 for p in self.params]
+        self.opt = AdamW(self.params, self._segments(self.pipe.avg), lr=lr, betas=betas, eps=eps, weight_decay=decays,
+                         state_bits=state_bits, master=self.params[0].dtype != torch.float32, max_norm=max_norm, seed=seed)
+
+    def _segments(self, avg: torch.Tensor):
+        return [avg[a:b] for a, b in zip(self.seg_off[:-1], self.seg_off[1:])]
+
+    def apply_average(self, avg: Optional[torch.Tensor] = None):
+        """Parameter-server update with the averaged reconstruction (Algorithm 1, last step); ``self.lr`` is looked up at every
+        step."""
+        avg = self.pipe.avg if avg is None else avg
+        self.opt.lr = self.lr
+        self.opt.step(None if avg is self._stepped else self._segments(avg))
+        self._stepped = avg

@@ -1,0 +1,571 @@
+"""The server's update on the GPU against the oracle: states bit for bit with the float32 statement of the step, weights within a
+bound that counts roundings of the float64 one, the norm within its one rounding."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import step as O
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+U = 2.0 ** -24                                      # a float32 rounding, relative
+HALF = {t: torch.finfo(t).eps / 2 for t in (F32, BF16, F16)}      # half a step, relative to the value
+TINY = {F32: 2.0 ** -149, BF16: 2.0 ** -134, F16: 2.0 ** -25}     # and among the subnormal numbers
+
+
+@pytest.fixture(scope="module")
+def co3():
+    import paper_2203_09044_amd as pkg
+    return pkg
+
+
+def scattered(values, dtype, skew, gap):
+    """Copies of arrays as views of one buffer, each begun ``skew`` elements off the place before it; the buffer, and a mask of
+    the places between."""
+    at, spans = skew, []
+    for x in values:
+        spans.append((at, at + x.size))
+        at += x.size + gap
+    flat = torch.full((at + 64,), 7.25, dtype=dtype, device="cuda")
+    between = torch.ones(at + 64, dtype=torch.bool, device="cuda")
+    for (a, b), x in zip(spans, values):
+        flat[a:b] = torch.from_numpy(x).cuda().to(dtype)
+        between[a:b] = False
+    return flat, between, [flat[a:b] for a, b in spans]
+
+
+def starts(sizes, bits):
+    unit = 256 if bits == 8 else 1
+    return np.concatenate([[0], np.cumsum([-(-n // unit) * unit for n in sizes])]).astype(int)
+
+
+def u8(t):
+    return t.view(torch.uint8).cpu().numpy()
+
+
+def states_of(opt):
+    """(m, v or r) as the float32 numbers they stand for, whole arrays."""
+    if opt.state_bits == 32:
+        return opt.m.cpu().numpy(), opt.v.cpu().numpy()
+    return O.decode(u8(opt.m), u8(opt.m_scale)), O.decode(u8(opt.r), u8(opt.r_scale))
+
+
+def check_step(opt, sizes, before, after_params, grads, masters_before, t, factor, lr, betas, eps, decays, scales, seed):
+    """States and weights after one step, from those before it."""
+    bits, at = opt.state_bits, starts(sizes, opt.state_bits)
+    m0, v0 = before
+    got_m, got_v = (u8(opt.m), u8(opt.r)) if bits == 8 else (opt.m.cpu().numpy(), opt.v.cpu().numpy())
+    want_scales = ([], [])
+    for k, n in enumerate(sizes):
+        a = at[k]
+        g = grads[k].astype(np.float32)
+        old_v = v0[a:a + n] * v0[a:a + n] if bits == 8 else v0[a:a + n]
+        m, v = O.moments32(m0[a:a + n], old_v, g, factor, *betas)
+        with np.errstate(all="ignore"):
+            root = np.sqrt(v)
+        if bits == 32:
+            assert np.array_equal(got_m[a:a + n].view(np.uint32), m.view(np.uint32)) or \
+                np.array_equal(got_m[a:a + n], m, equal_nan=True), ("m", k)
+            assert np.array_equal(got_v[a:a + n], v, equal_nan=True), ("v", k)
+        else:
+            pad = at[k + 1] - a
+            r16 = O.random16(a, pad, seed, t)
+            mc, ms = O.encode(np.pad(m, (0, pad - n)), r16, False)
+            rc, rs = O.encode(np.pad(root, (0, pad - n)), 65535 - r16, True)
+            assert np.array_equal(got_m[a:a + n], mc[:n]), ("m", k)
+            assert np.array_equal(got_v[a:a + n], rc[:n]), ("r", k)
+            assert np.array_equal(u8(opt.m_scale)[a // 256:at[k + 1] // 256], ms), ("m_scale", k)
+            assert np.array_equal(u8(opt.r_scale)[a // 256:at[k + 1] // 256], rs), ("r_scale", k)
+        # from the new moments on: root 1/2, rbc2 1/2 and its product 1/2, eps 1/2 and the sum 1/2 (all of one sign), the quotient
+        # 1/2, the factor of the step 1/2, lr_scale 1/2 and 1/2 for the product: 4.5 roundings of the step's part, 7 with a unit in
+        # the last place for the root and the quotient each; lr, lr_scale, decay and products: 3 of the decay's; their sum and
+        # the last difference one each
+        with np.errstate(all="ignore"):
+            w, decay, step = O.weight64(masters_before[k], m, None, t, lr * scales[k], *betas, eps, decays[k], root=root)
+        bound = U * (1 + 1e-5) * (np.abs(w) + np.abs(decay + step) + 7 * np.abs(step) + 3 * np.abs(decay)) + 2.0 ** -148
+        fine = np.isfinite(w)
+        if opt.master is not None:
+            got = opt.master[a:a + n].double().cpu().numpy()
+            assert np.all(np.abs(got - w)[fine] <= bound[fine]), ("master", k)
+            assert np.array_equal(after_params[k], torch.from_numpy(got).float().to(opt._table.params[0].dtype).float().numpy(),
+                                  equal_nan=True), ("param", k)
+        else:
+            dt = opt._table.params[0].dtype
+            room = bound if dt == F32 else bound + HALF[dt] * (np.abs(w) + bound) + TINY[dt]
+            far = np.abs(after_params[k].astype(np.float64) - w)
+            over = fine & (np.abs(w) < float(torch.finfo(dt).max))
+            assert np.all(far[over] <= room[over]), ("param", k, float(np.max((far / room)[over])))
+        assert np.array_equal(np.isnan(after_params[k]), np.isnan(w)), k
+
+
+TABLES = {"one": [1], "tiny": [3, 0, 5, 1, 2], "blocks": [255, 256, 257, 1, 0, 511, 512, 513], "chunks": [1023, 1024, 1025, 4095, 4097],
+          "mixed": [10_000, 64, 64, 1, 70_003, 0, 10]}
+TYPES = [(F32, F32, False), (F32, BF16, False), (BF16, BF16, False), (BF16, F32, True), (F16, F16, True), (F16, F32, False)]
+
+
+def run_steps(co3, sizes, ptype, gtype, master, bits, steps=3, skew=0, gap=0, max_norm=None, lr=2e-3, betas=(0.9, 0.98), eps=1e-6,
+              seed=0x123456789AB, grad_scale=1.0, first=0, gradients=None, **kw):
+    rng = np.random.default_rng(sum(sizes) + bits)
+    decays = [0.1 if k % 2 else 0.0 for k in range(len(sizes))]
+    scales = [1.0 if k % 3 else 0.5 for k in range(len(sizes))]
+    p0 = [(rng.standard_normal(n) * 0.1).astype(np.float32) for n in sizes]
+    spread = [10.0 ** rng.uniform(-4, 0) for _ in sizes]
+    flat_p, between_p, params = scattered(p0, ptype, skew, gap)
+    flat_g, between_g, grads = scattered([np.zeros(n, np.float32) for n in sizes], gtype, skew + 1, gap)
+    opt = co3.AdamW(params, grads, lr=lr, betas=betas, eps=eps, weight_decay=decays, lr_scales=scales, state_bits=bits, master=master,
+                    max_norm=max_norm, seed=seed, grad_scale=grad_scale, **kw)
+    opt.t = first
+    at = starts(sizes, bits)
+    marks = torch.ones(opt.m.numel(), dtype=torch.bool)            # the places behind a tensor's last element
+    for a, n in zip(at, sizes):
+        marks[a:a + n] = False
+    if bits == 8:
+        for s in (opt.m, opt.r):
+            s.view(torch.uint8)[marks.cuda()] = 0x55
+    for t in range(first + 1, first + steps + 1):
+        for k, g in enumerate(grads):
+            x = rng.standard_normal(sizes[k]) * np.exp(rng.standard_normal(sizes[k])) * spread[k] if gradients is None else gradients(t, k, sizes[k])
+            x[rng.random(sizes[k]) < 0.1] = 0.0
+            g.copy_(torch.from_numpy(np.asarray(x, np.float32)).cuda().to(gtype))
+        hg = [g.float().cpu().numpy() for g in grads]
+        before = states_of(opt)
+        if bits == 8:
+            before = tuple(np.where(marks.numpy(), 0, s) for s in before)
+        if opt.master is not None:
+            wb = [opt.master[a:a + n].cpu().numpy() for a, n in zip(at, sizes)]
+        else:
+            wb = [p.float().cpu().numpy() for p in params]
+        opt.step()
+        factor = np.float32(grad_scale)
+        if max_norm is not None:
+            norm, c = O.norm(hg, grad_scale, max_norm)
+            got = opt.norm.cpu().numpy()
+            assert abs(got[0] - norm) <= U * (1 + 1e-6) * norm and abs(got[1] - c) <= U * (1 + 1e-6) * c
+            factor = got[1]
+        assert opt.t == t
+        check_step(opt, sizes, before, [p.float().cpu().numpy() for p in params], hg, wb, t, factor, lr, betas, eps, decays, scales, seed)
+        assert bool((flat_p[between_p] == 7.25).all()) and bool((flat_g[between_g] == 7.25).all())
+        if bits == 8:
+            for s in (opt.m, opt.r):
+                assert bool((s.view(torch.uint8)[marks.cuda()] == 0x55).all())
+    return opt
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("table", sorted(TABLES))
+@pytest.mark.parametrize("ptype,gtype,master", TYPES)
+def test_steps_of_every_type(co3, bits, table, ptype, gtype, master):
+    run_steps(co3, TABLES[table], ptype, gtype, master, bits)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("ptype,gtype,master", [(F32, F16, False), (BF16, F16, False), (BF16, BF16, True), (F16, BF16, True), (F16, F16, False), (F16, F32, True)])
+@pytest.mark.parametrize("skew,gap", [(1, 0), (3, 1), (2, 5)])
+def test_tensors_begin_at_any_element(co3, bits, ptype, gtype, master, skew, gap):
+    run_steps(co3, TABLES["blocks"] + [2049], ptype, gtype, master, bits, steps=2, skew=skew, gap=gap)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("max_norm,grad_scale", [(1.0, 1.0), (1e-3, 0.25), (1e9, 8.0)])
+def test_clipped_and_scaled_steps(co3, bits, max_norm, grad_scale):
+    run_steps(co3, TABLES["mixed"], F32, F32, False, bits, max_norm=max_norm, grad_scale=grad_scale)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_long_tensors_and_late_steps(co3, bits):
+    """Sizes on the longer chunks; a step number whose powers need many factors."""
+    run_steps(co3, [4_200_001, 5, 70_000], F32, F32, False, bits, steps=1, skew=1)
+    run_steps(co3, [5000], BF16, F32, False, bits, steps=2, first=1_234_567)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_from_subnormal_to_huge(co3, bits):
+    def gradients(t, k, n):
+        return np.random.default_rng(t).standard_normal(n) * 10.0 ** np.random.default_rng(k + t).uniform(-42, 15, n)
+    run_steps(co3, [2000, 300], F32, F32, False, bits, gradients=gradients)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("betas", [(0.0, 0.0), (0.0, 0.999), (0.95, 0.0)])
+def test_betas_of_zero(co3, bits, betas):
+    run_steps(co3, [700, 3], F32, F32, False, bits, betas=betas)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_a_gradient_that_is_not_finite_stays_in_its_block(co3, bits, bad):
+    """Without a norm the step is taken: the element itself is lost, with 8-bit states those that share its scale
+    from the next step on, nothing else."""
+    sizes = [2000, 512]
+
+    def gradients(t, k, n):
+        x = np.random.default_rng(t * 7 + k).standard_normal(n)
+        if k == 0 and t == 2:
+            x[300] = bad
+        return x
+    rng_free = [(0.1 * np.random.default_rng(k).standard_normal(n)).astype(np.float32) for k, n in enumerate(sizes)]
+    runs = []
+    for poisoned in (False, True):
+        params = [torch.from_numpy(x.copy()).cuda() for x in rng_free]
+        grads = [torch.zeros_like(p) for p in params]
+        opt = co3.AdamW(params, grads, state_bits=bits, seed=3)
+        for t in range(1, 5):
+            for k, g in enumerate(grads):
+                x = gradients(t, k, sizes[k])
+                g.copy_(torch.from_numpy(x if poisoned else np.where(np.isfinite(x), x, 0.5)))
+            opt.step()
+        runs.append((opt, params))
+    touched = torch.zeros(2000, dtype=torch.bool, device="cuda")
+    if bits == 8:
+        touched[256:512] = True
+    else:
+        touched[300] = True
+    (a, pa), (b, pb) = runs
+    assert torch.equal(pa[0][~touched], pb[0][~touched]) and torch.equal(pa[1], pb[1])
+    assert not bool(torch.isfinite(pb[0][300]))
+    for x, y in zip(a.moments(), b.moments()):
+        assert x[0].shape == y[0].shape
+    assert torch.equal(a.moments()[1][0], b.moments()[1][0]) and torch.equal(a.moments()[0][1][~touched], b.moments()[0][1][~touched])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_norm_that_is_not_finite_leaves_everything(co3, bits):
+    params = [torch.randn(3000, device="cuda"), torch.randn(5, device="cuda")]
+    grads = [torch.randn_like(p) for p in params]
+    opt = co3.AdamW(params, grads, state_bits=bits, max_norm=1.0)
+    opt.step()
+    keep = [p.clone() for p in params] + [s.view(torch.uint8).clone() for s in opt._named().values()]
+    for bad in (math.nan, math.inf, -math.inf):
+        grads[1][2] = bad
+        opt.step()
+        assert float(opt.norm[1]) == -1.0 and not math.isfinite(float(opt.norm[0]))
+        now = params + [s.view(torch.uint8) for s in opt._named().values()]
+        assert all(torch.equal(x, y) for x, y in zip(keep, now))
+    assert opt.t == 1 and opt.skipped == 3
+    grads[1][2] = 0.5
+    opt.step()
+    assert opt.t == 2 and opt.skipped == 3 and not torch.equal(keep[0], params[0])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("sizes", [[1], [0], [0, 1, 0], [3, 255, 4097], [5_000_003, 2], [64] * 3000])
+@pytest.mark.parametrize("skew", [0, 1])
+def test_norm(co3, dtype, sizes, skew):
+    rng = np.random.default_rng(len(sizes))
+    _, _, grads = scattered([rng.standard_normal(n).astype(np.float32) * 0.01 for n in sizes], dtype, skew, 0)
+    for max_norm, scale in ((1.0, 1.0), (1e6, 1.0), (1e-2, 0.5), (math.inf, 4.0)):
+        out = co3.GradNorm(grads, max_norm=max_norm, grad_scale=scale).compute().cpu().numpy()
+        norm, c = O.norm([g.double().cpu().numpy() for g in grads], scale, max_norm)
+        # squares of numbers of 24 bits are exact in 53, their sum in any order within 2^-53 an addition: one rounding to fp32 remains
+        assert abs(out[0] - norm) <= U * (1 + 1e-6) * norm and abs(out[1] - c) <= U * (1 + 1e-6) * c
+
+
+def test_norm_at_the_ends_of_the_range(co3):
+    big = torch.full((1000,), 3e38, device="cuda")
+    out = co3.GradNorm([big], max_norm=1.0).compute()
+    assert math.isinf(float(out[0])) and float(out[1]) > 0          # beyond float32, but a number
+    assert abs(float(out[1]) * 3e38 * math.sqrt(1000.0) - 1.0) < 1e-2
+    small = torch.full((10,), 1e-45, device="cuda")
+    out = co3.GradNorm([small], max_norm=1.0).compute()
+    assert float(out[0]) == pytest.approx(2.0 ** -149 * math.sqrt(10.0), rel=0.2) and float(out[1]) == 1.0
+    for bad in (math.inf, math.nan):
+        small[3] = bad
+        assert float(co3.GradNorm([small]).compute()[1]) == -1.0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_equal_calls_give_equal_results(co3, bits):
+    def run():
+        torch.manual_seed(0)
+        params = [torch.randn(n, device="cuda") for n in (100_000, 3, 5_000_000)]
+        grads = [torch.randn_like(p) for p in params]
+        opt = co3.AdamW(params, grads, state_bits=bits, max_norm=1.0, seed=9)
+        for _ in range(3):
+            opt.step()
+        return params + [s.view(torch.uint8) for s in opt._named().values()]
+    assert all(torch.equal(a, b) for a, b in zip(run(), run()))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("how", ["device_steps", "tensor_lr"])
+def test_the_devices_count_is_the_hosts(co3, bits, how):
+    results = []
+    for device in (False, True):
+        torch.manual_seed(1)
+        params = [torch.randn(5000, device="cuda")]
+        grads = [torch.randn_like(params[0])]
+        lr = torch.tensor([1e-3], device="cuda") if device and how == "tensor_lr" else 1e-3
+        opt = co3.AdamW(params, grads, lr=float(torch.tensor(1e-3)) if not device and how == "tensor_lr" else lr, state_bits=bits,
+                        device_steps=device, seed=5)
+        for _ in range(4):
+            opt.step()
+        assert opt.t == 4
+        results.append(params + [s.view(torch.uint8) for s in opt._named().values()])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("bits,ptype,max_norm", [(32, F32, None), (8, F32, 1.0), (8, BF16, 1.0), (32, BF16, 0.5)])
+def test_replays_of_a_captured_step_equal_eager_ones(co3, bits, ptype, max_norm):
+    def make():
+        torch.manual_seed(2)
+        params = [torch.randn(n, device="cuda").to(ptype) for n in (40_000, 7, 300)]
+        grads = [torch.zeros_like(p) for p in params]
+        lr = torch.tensor([1e-3], device="cuda")
+        return params, grads, lr, co3.AdamW(params, grads, lr=lr, state_bits=bits, max_norm=max_norm, master=ptype != F32, device_steps=True, seed=4)
+    pe, ge, le, eager = make()
+    pg, gg, lg, graphed = make()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        graphed.step()
+    assert graphed.t == 0                               # capturing runs nothing
+    for t in range(1, 6):
+        for a, b in zip(ge, gg):
+            a.copy_(torch.randn_like(a))
+            if t == 3 and max_norm is not None:
+                a[0] = math.nan                         # a step that is left out, in the middle
+            b.copy_(a)
+        for lr in (le, lg):
+            lr.fill_(1e-3 / t)
+        eager.step()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.rand(1 << 20, device="cuda").sum().item() > 0
+        assert graphed.t == eager.t == (t - 1 if t >= 3 and max_norm is not None else t)
+        for a, b in zip(pe + list(eager._named().values()) + [eager.norm], pg + list(graphed._named().values()) + [graphed.norm]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), t
+
+
+def test_a_step_counted_by_the_host_is_not_captured(co3):
+    p, g = torch.zeros(64, device="cuda"), torch.zeros(64, device="cuda")
+    opt = co3.AdamW([p], [g])
+    opt.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        q = p + 1                                       # a graph has to hold something
+        with pytest.raises(RuntimeError):
+            opt.step()
+    assert opt.t == 1 and q is not None
+
+
+def test_steps_on_two_streams_at_once(co3):
+    def make(seed):
+        torch.manual_seed(seed)
+        params = [torch.randn(300_000 + seed, device="cuda"), torch.randn(11, device="cuda")]
+        return params, co3.AdamW(params, [torch.randn_like(p) for p in params], state_bits=8 if seed else 32, max_norm=0.7, seed=seed)
+    alone = [make(s) for s in (0, 1)]
+    for _, opt in alone:
+        for _ in range(4):
+            opt.step()
+    both = [make(s) for s in (0, 1)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(4):
+        for (_, opt), s in zip(both, streams):
+            with torch.cuda.stream(s):
+                opt.step()
+    torch.cuda.synchronize()
+    for (pa, a), (pb, b) in zip(alone, both):
+        assert all(torch.equal(x, y) for x, y in zip(pa, pb))
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a._named().values(), b._named().values()))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_tensors_that_move_and_gradients_that_change(co3, bits):
+    torch.manual_seed(3)
+    ref_p = [torch.randn(1000, device="cuda"), torch.randn(30, device="cuda")]
+    ref = co3.AdamW(ref_p, [torch.zeros_like(p) for p in ref_p], state_bits=bits, seed=1)
+    p = [torch.nn.Parameter(x.clone()) for x in ref_p]
+    opt = co3.AdamW(p, [torch.zeros_like(x) for x in p], state_bits=bits, seed=1)
+    for t in range(4):
+        g = [torch.randn_like(x) for x in ref_p]
+        for a, b in zip(ref._table.grads, g):
+            a.copy_(b)
+        ref.step()
+        if t == 2:
+            p[0].data = p[0].data.clone()               # the parameter's memory is another one now
+        opt.step(g)                                     # new gradient tensors at every step
+        for a, b in zip(ref_p, p):
+            assert torch.equal(a, b.detach())
+    with pytest.raises(ValueError):
+        opt.step([torch.zeros(1000, device="cuda")])
+    with pytest.raises(ValueError):
+        opt.step([torch.zeros(1000, device="cuda"), torch.zeros(31, device="cuda")])
+    with pytest.raises(ValueError):
+        opt.step([torch.zeros(1000), torch.zeros(30)])
+    opt.step([x.to(BF16) for x in ref._table.grads])    # of another type
+    assert opt.t == 5
+
+
+@pytest.mark.parametrize("bits,ptype", [(32, F32), (8, F32), (8, BF16)])
+def test_a_saved_state_goes_on_as_the_run_does(co3, bits, ptype):
+    def make(p):
+        return co3.AdamW(p, [torch.zeros_like(x) for x in p], state_bits=bits, master=ptype != F32, seed=6, max_norm=1.0 if bits == 8 else None)
+    torch.manual_seed(4)
+    a = [torch.randn(700, device="cuda").to(ptype), torch.randn(3, device="cuda").to(ptype)]
+    opt = make(a)
+    gs = [[torch.randn_like(x) for x in a] for _ in range(6)]
+    for g in gs[:3]:
+        opt.step(g)
+    saved, b = opt.state_dict(), [x.clone() for x in a]
+    other = make(b)
+    other.load_state_dict(saved)
+    for g in gs[3:]:
+        opt.step(g)
+        other.step(g)
+    assert all(torch.equal(x, y) for x, y in zip(a, b)) and opt.t == other.t == 6
+    with pytest.raises(ValueError):
+        co3.AdamW(b, gs[0], state_bits=40 - bits).load_state_dict(saved)
+
+
+def test_tensors_of_no_elements(co3):
+    p = [torch.zeros(0, device="cuda"), torch.zeros(0, device="cuda")]
+    for bits in (32, 8):
+        opt = co3.AdamW(p, [torch.zeros_like(x) for x in p], state_bits=bits, max_norm=1.0)
+        opt.step()
+        assert opt.t == 1 and opt.norm.tolist() == [0.0, 1.0]
+        co3.AdamW(p, [torch.zeros_like(x) for x in p], state_bits=bits).step()
+    assert co3.GradNorm(p, max_norm=2.0).compute().tolist() == [0.0, 1.0]
+
+
+def test_refusals(co3):
+    x = torch.zeros(8, 4, device="cuda")
+    z = torch.zeros(8, 4, device="cuda")
+    for params, grads, kw in (([x.t()], [z], {}), ([x], [z.t()], {}), ([x, x.half()], [z, z.clone()], {}), ([x], [z, z], {}),
+                              ([x], [z[:4]], {}), ([x.double()], [z], {}), ([x], [z.long()], {}), ([x, x], [z, z], {}), ([x], [x], {}),
+                              ([x[:4], x[2:6]], [z[:4], z[4:]], {}), ([x], [z], dict(master=True)), ([x], [z], dict(weight_decay=[0.1, 0.1])),
+                              ([x], [z], dict(weight_decay=-0.1)), ([x], [z], dict(lr_scales=[math.nan])), ([x], [z], dict(lr=-1.0)),
+                              ([x], [z], dict(lr=math.nan)), ([x], [z], dict(lr=torch.tensor([1e-3]))), ([x], [z.cpu()], {}), ([], [], {})):
+        with pytest.raises(ValueError):
+            co3.AdamW(params, grads, **kw)
+    B = co3.binding
+    opt = co3.AdamW([x], [z])
+    t = opt._table
+    for m in (opt.m[:31], opt.m.half(), opt.m.cpu()):
+        with pytest.raises((ValueError, TypeError)):
+            B.adamw(t.layout, t.plan, m, opt.v, opt._args)
+    with pytest.raises(ValueError):
+        B.grad_norm(t.layout, t.plan[:8], 1.0, 1.0, torch.zeros(2, device="cuda"), torch.zeros(1, dtype=torch.float64, device="cuda"))
+    with pytest.raises(ValueError):
+        B.step_begin(opt._args, torch.zeros(63, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        B.step_begin(opt._args, torch.zeros(64, dtype=torch.uint8, device="cuda"), torch.zeros(4, dtype=torch.float64, device="cuda"), count=5)
+
+
+def test_the_separate_calls_make_the_step(co3):
+    """Two tables (parameters of two types) under one norm: the calls that the handle makes, made by hand."""
+    B = co3.binding
+    torch.manual_seed(7)
+    groups = [[torch.randn(3000, device="cuda"), torch.randn(5, device="cuda")], [torch.randn(2000, device="cuda").to(BF16)]]
+    grads = [[torch.randn_like(p) for p in group] for group in groups]
+    opts = [co3.AdamW(p, g, state_bits=b) for p, g, b in zip(groups, grads, (32, 8))]
+    partials = torch.zeros(sum(o._table.layout.partials for o in opts), dtype=torch.float64, device="cuda")
+    state = torch.zeros(64, dtype=torch.uint8, device="cuda")
+    args = B.AdamwArgs(1e-3, 0.9, 0.999, 1e-8, 1.0, 0.5, 0, 11)
+    want_p = [[p.float().cpu().numpy() for p in group] for group in groups]
+    at = 0
+    for o in opts:
+        n = o._table.layout.partials
+        B.grad_sumsq(o._table.layout, o._table.plan, partials[at:at + n])
+        at += n
+    B.step_begin(args, state, partials)
+    a, b = opts
+    B.adamw(a._table.layout, a._table.plan, a.m, a.v, args, state=state)
+    B.adamw8(b._table.layout, b._table.plan, b.m, b.m_scale, b.r, b.r_scale, args, state=state)
+    norm, c = O.norm([g.double().cpu().numpy() for gs in grads for g in gs], 1.0, 0.5)
+    got = state.view(torch.float32)[4:6].cpu().numpy()
+    assert abs(got[0] - norm) <= U * (1 + 1e-6) * norm and abs(got[1] - c) <= U * (1 + 1e-6) * c
+    for o, p, g, before in zip(opts, groups, grads, want_p):
+        sizes = [x.numel() for x in p]
+        zero = np.zeros(o.m.numel(), np.float32)
+        check_step(o, sizes, (zero, zero), [x.float().cpu().numpy() for x in p], [x.float().cpu().numpy() for x in g], before, 1, got[1],
+                   1e-3, (0.9, 0.999), 1e-8, [0.01] * len(sizes), [1.0] * len(sizes), 11)
+
+
+@pytest.mark.parametrize("bits,ptype,n", [(32, F32, (1 << 30) + 1027), (8, BF16, (1 << 31) + 1300)])
+def test_offsets_beyond_32_bits(co3, bits, ptype, n):
+    """One tensor whose arrays are longer than 2^32 bytes (the parameters; with 8-bit states the states' places pass 2^31): its
+    ends and the places around the limits, block by block against the oracle."""
+    p = torch.empty(n, dtype=ptype, device="cuda").normal_()
+    g = torch.empty(n, dtype=ptype, device="cuda").normal_()
+    opt = co3.AdamW([p], [g], state_bits=bits, weight_decay=0.0, lr=1e-2, seed=1 << 33)
+    spots = [(a, min(a + 2048, n)) for a in (0, (1 << 29) - 1024, (1 << 30) - 1024, (1 << 31) - 1024, n - n % 256 - 1024) if a < n]
+    before = [p[a:b].float().cpu().numpy() for a, b in spots]
+    hg = [g[a:b].float().cpu().numpy() for a, b in spots]
+    opt.step()
+    for (a, b), w0, x in zip(spots, before, hg):
+        m, v = O.moments32(np.zeros(b - a, np.float32), np.zeros(b - a, np.float32), x, 1.0, 0.9, 0.999)
+        if bits == 32:
+            assert np.array_equal(opt.m[a:b].cpu().numpy(), m) and np.array_equal(opt.v[a:b].cpu().numpy(), v)
+        else:
+            pad = -(b - a) % 256
+            r16 = O.random16(a, b - a + pad, 1 << 33, 1)
+            mc, ms = O.encode(np.pad(m, (0, pad)), r16, False)
+            rc, rs = O.encode(np.pad(np.sqrt(v), (0, pad)), 65535 - r16, True)
+            assert np.array_equal(u8(opt.m[a:b]), mc[:b - a]) and np.array_equal(u8(opt.r[a:b]), rc[:b - a])
+            assert np.array_equal(u8(opt.m_scale)[a // 256:a // 256 + len(ms)], ms)
+            assert np.array_equal(u8(opt.r_scale)[a // 256:a // 256 + len(rs)], rs)
+        w, decay, step = O.weight64(w0, m, v, 1, 1e-2, 0.9, 0.999, 1e-8, 0.0)
+        bound = U * (1 + 1e-5) * (np.abs(w) + 9 * np.abs(step)) + 2.0 ** -148
+        room = bound if ptype == F32 else bound + HALF[ptype] * (np.abs(w) + bound) + TINY[ptype]
+        assert np.all(np.abs(p[a:b].double().cpu().numpy() - w) <= room)
+    del p, g, opt
+    torch.cuda.empty_cache()
+
+
+# ---- the framework's own path ---------------------------------------------------------------------------------------
+def problem(dtype=F32):
+    torch.manual_seed(12)
+    model = torch.nn.Sequential(torch.nn.Linear(48, 300), torch.nn.ReLU(), torch.nn.Linear(300, 10)).cuda().to(dtype)
+
+    def sample(t, u):
+        gen = torch.Generator().manual_seed(100 * t + u)
+        return torch.randn(32, 48, generator=gen).cuda().to(dtype), torch.randint(0, 10, (32,), generator=gen).cuda()
+    return model, sample
+
+
+@pytest.mark.parametrize("bits,max_norm,dtype", [(32, None, F32), (32, 0.5, F32), (8, 0.5, F32), (8, None, F32), (32, 0.5, BF16), (8, 0.5, BF16)])
+def test_training_steps_the_model_with_the_averaged_reconstruction(co3, bits, max_norm, dtype):
+    """Algorithm 1 with AdamW as the server's update: users' gradients through the codec, the average clipped, every tensor of
+    the model stepped; several iterations, each checked from the state before it."""
+    model, sample = problem(dtype)
+    users = 3
+    opt = co3.Co3AdamW(model, users, co3.Fmt(4, 3), lr=1e-2, weight_decay=0.1, state_bits=bits, max_norm=max_norm, seed=21)
+    sizes, at = opt.sizes, starts(opt.sizes, bits)
+    decays = [0.1 if p.dim() > 1 else 0.0 for p in opt.params]
+    loss = lambda y, c: torch.nn.functional.cross_entropy(y.float(), c)  # noqa: E731
+    for t in range(1, 4):
+        before = states_of(opt.opt)
+        if opt.opt.master is not None:
+            w = [opt.opt.master[a:a + n].cpu().numpy() for a, n in zip(at, sizes)]
+        else:
+            w = [p.detach().reshape(-1).cpu().numpy().copy() for p in opt.params]
+        opt.step([sample(t, u) for u in range(users)], loss)
+        avg = opt.pipe.avg[:opt.n].cpu().numpy()
+        grads = [avg[a:b] for a, b in zip(opt.seg_off[:-1], opt.seg_off[1:])]
+        factor = np.float32(1.0)
+        if max_norm is not None:
+            norm, c = O.norm(grads, 1.0, max_norm)
+            factor = opt.opt.norm.cpu().numpy()[1]
+            assert abs(factor - c) <= U * (1 + 1e-6) * c
+        check_step(opt.opt, sizes, before, [p.detach().reshape(-1).float().cpu().numpy() for p in opt.params], grads, w, t, factor, 1e-2,
+                   (0.9, 0.999), 1e-8, decays, [1.0] * len(sizes), 21)
+    assert opt.opt.t == 3
+
+
+def test_training_with_another_average_and_rate(co3):
+    model, sample = problem()
+    opt = co3.Co3AdamW(model, 2, co3.Fmt(3, 1), lr=1e-2)
+    ref, _ = problem()
+    torch.manual_seed(0)
+    avgs = [torch.randn(opt.n, device="cuda") for _ in range(3)]
+    other = co3.AdamW(list(ref.parameters()), [torch.zeros_like(p) for p in ref.parameters()], lr=1e-2,
+                      weight_decay=[0.01 if p.dim() > 1 else 0.0 for p in ref.parameters()])
+    for k, avg in enumerate(avgs):
+        opt.lr = other.lr = 1e-2 / (k + 1)
+        opt.apply_average(avg)
+        other.step([avg[a:b] for a, b in zip(opt.seg_off[:-1], opt.seg_off[1:])])
+    assert all(torch.equal(a.detach(), b.detach()) for a, b in zip(model.parameters(), ref.parameters()))
