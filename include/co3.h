@@ -407,7 +407,8 @@ void co3_set_exchange_spin_limit(int64_t polls);
  * Step t, every operation on its own rounded to fp32, scalars computed in fp64 and rounded once:
  *     g' = factor * g;   m' = beta1 m + (1 - beta1) g';   v' = beta2 v + (1 - beta2) (g' g')
  *     p' = p - ((lr_s weight_decay) p + (lr_s / (1 - beta1^t)) (m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)))
- * with lr_s = lr * lr_scale of the tensor (sqrt and the quotient are correctly rounded).  Parameters and gradients are
+ * with lr_s = lr * lr_scale of the tensor (sqrt correctly rounded, the quotient by 1 / sqrt(1 - beta2^t) a product, that by the
+ * divisor within two units in the last place).  Parameters and gradients are
  * fp32, bf16 or fp16; a 16-bit parameter is rounded to nearest, ties to even, from the fp32 result, and the step starts
  * from it, or, where a master array is given, from the fp32 value kept there (the parameter is then written only).
  *
@@ -421,7 +422,7 @@ void co3_set_exchange_spin_limit(int64_t polls);
  * that is cut off rounds the number up with its own probability: by 16 bits of a hash of (seed, t, place), the
  * complement of m's for r, so that equal calls give equal results.  (Rounding to nearest would hold r where it is: a
  * step moves v by some 1 - beta2 of itself, the next number is 12 % away.)  An r that is not zero does not become zero.
- * Where a gradient is not finite its block's states become infinite.
+ * Where a gradient is not finite, its block's states are not either, or no longer say anything.
  */
 #define CO3_F32 0
 #define CO3_BF16 1
@@ -446,14 +447,14 @@ typedef struct {
     int64_t blocks;         /* scales of each 8-bit state, 0 with 32-bit states */
     int64_t chunks;         /* entries of the plan */
     int64_t plan_bytes;     /* bytes of the plan, at least 16 */
-    int64_t partials;       /* partial sums (double) that a norm needs, at least 1 */
+    int64_t partials;       /* doubles of workspace that a norm needs */
     int32_t param_type, grad_type;
     int32_t state_bits;     /* 32, 8, or 0 for a norm alone */
-    int32_t chunk;          /* elements of a tensor that one workgroup takes */
+    int32_t chunk;          /* places that an entry spans at most */
 } co3_step_layout;
 
 typedef struct {
-    double lr, beta1, beta2, eps; /* lr >= 0, 0 <= beta < 1, eps > 0 also in fp32 */
+    double lr, beta1, beta2, eps; /* lr >= 0, 0 <= beta < 1, eps >= 2^-126 in fp32 */
     double grad_scale;            /* multiplies every gradient, > 0 (1: as they are) */
     double max_norm;              /* > 0; the norm beyond which gradients are scaled down (INFINITY: never) */
     int64_t t;                    /* number of this step, from 1; used where no co3_step_state is given */
@@ -480,27 +481,33 @@ int32_t co3_step_layout_of(const co3_step_tensor *tensors_host, int32_t T, int32
 int32_t co3_step_plan(const co3_step_tensor *tensors_host, int32_t T, const co3_step_layout *layout_host, void *plan_host,
                       size_t plan_bytes);
 
-/* partials[layout->partials] = sums of squares, in fp64, of the gradients of a plan (one launch).  Several tables, as of
- * models with parameters of several types, write one behind another and are finished together. */
+/*
+ * Sums of squares, in fp64, of the gradients of a plan: one launch.  partials [layout->partials] double, zeroed once by the caller; calls
+ * that may run at the same time must not share them.  Several tables, as of models with parameters of several types,
+ * write one behind another and are finished together by co3_step_begin.
+ */
 int32_t co3_grad_sumsq(const co3_step_layout *layout_host, const void *plan, double *partials, void *stream);
 
 /*
- * Global norm of the gradients of a plan, and the factor that clips it:
+ * Global norm of the gradients of a plan, and the factor that clips it, in one launch:
  *     out[0] = norm = grad_scale * sqrt(sum g^2),   out[1] = grad_scale * min(1, max_norm / (norm + 1e-6))
- * out[1] is -1 where the sum is not finite.  partials: layout->partials doubles of workspace.  The sums are taken in a
- * fixed order: equal calls give equal results.
+ * out[1] is -1 where the sum is not finite.  partials: workspace as of co3_grad_sumsq.  The sums are taken in a fixed order: equal
+ * calls give equal results.
  */
 int32_t co3_grad_norm(const co3_step_layout *layout_host, const void *plan, double grad_scale, double max_norm, float *out,
                       double *partials, void *stream);
 
 /*
  * Begins a step that the device counts (for captured steps, clipped ones, learning rates that the device holds).
- * partials: NULL (no norm is taken, the factor is grad_scale), or count sums of co3_grad_sumsq, from which norm and factor
- * follow as in co3_grad_norm.  If the norm is not finite, state->skipped goes up, and the step that follows changes
- * nothing; else state->t goes up.  lr_dev: NULL, or a device float that stands for args->lr.
+ * co3_step_begin: partials NULL (no norm is taken, the factor is grad_scale), or count doubles that calls of co3_grad_sumsq have
+ * filled, from which norm and factor follow as in co3_grad_norm.  co3_step_begin_norm: the norm is that of the gradients of
+ * the plan, taken in the same launch (partials: workspace).  If the norm is not finite, state->skipped goes up, and the
+ * step that follows changes nothing; else state->t goes up.  lr_dev: NULL, or a device float that stands for args->lr.
  */
 int32_t co3_step_begin(const co3_adamw_args *args_host, const double *partials, int64_t count, const float *lr_dev,
                        co3_step_state *state, void *stream);
+int32_t co3_step_begin_norm(const co3_step_layout *layout_host, const void *plan, const co3_adamw_args *args_host, double *partials,
+                            const float *lr_dev, co3_step_state *state, void *stream);
 
 /*
  * AdamW on all tensors of a plan, with 32-bit (co3_adamw) or 8-bit states (co3_adamw8): one launch.

@@ -77,7 +77,7 @@ def encode(x, r16, keep):
     s = np.clip(np.where(top == 0.0, 0, s), 0, 247)
     s = np.where(np.isfinite(top), s, 247)
     y = np.ldexp(a, 127 - s[:, None]).reshape(-1)
-    y = np.where(y < 2.0 ** -6, np.rint(np.ldexp(np.minimum(y, 1.0), 29)) * 2.0 ** -29, y)       # 20 bits below a code, here too
+    y = np.where(y < 2.0 ** -6, np.floor(np.ldexp(np.minimum(y, 1.0), 29)) * 2.0 ** -29, y)      # 20 bits below a code, here too
     lo = np.clip(np.searchsorted(E4M3, y, side="right") - 1, 0, 126)
     gap = np.append(np.diff(E4M3), np.inf)[lo]
     with np.errstate(invalid="ignore"):

@@ -31,7 +31,8 @@ EXPORTS = (
     "co3_convert_encode_workspace_bytes", "co3_convert_encode", "co3_convert_encode_layers", "co3_encode_static",
     "co3_user_encode_workspace_bytes", "co3_user_encode", "co3_set_exchange_spin_limit", "co3_design_layer_tables",
     "co3_ps_aggregate_partial", "co3_ps_decode_users", "co3_ps_average",
-    "co3_step_layout_of", "co3_step_plan", "co3_grad_sumsq", "co3_grad_norm", "co3_step_begin", "co3_adamw", "co3_adamw8",
+    "co3_step_layout_of", "co3_step_plan", "co3_grad_sumsq", "co3_grad_norm", "co3_step_begin",
+    "co3_step_begin_norm", "co3_adamw", "co3_adamw8",
 )
 KERNEL_COUNT = 17
 TYPE_OF = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # CO3_F32, CO3_BF16, CO3_F16
@@ -163,6 +164,8 @@ def _load():
     L.co3_grad_norm.argtypes = [lay, p, C.c_double, C.c_double, p, p, p]
     L.co3_step_begin.restype = i32
     L.co3_step_begin.argtypes = [arg, p, i64, p, p, p]
+    L.co3_step_begin_norm.restype = i32
+    L.co3_step_begin_norm.argtypes = [lay, p, arg, p, p, p, p]
     L.co3_adamw.restype = i32
     L.co3_adamw.argtypes = [lay, p, p, p, p, arg, p, p]
     L.co3_adamw8.restype = i32
@@ -539,7 +542,7 @@ def grad_sumsq(layout: StepLayout, plan, partials, stream=None):
 
 
 def grad_norm(layout: StepLayout, plan, grad_scale: float, max_norm: float, out, partials, stream=None):
-    """out: 2 float32 on the device (norm, factor); partials: float64 workspace."""
+    """out: 2 float32 on the device (norm, factor); partials: float64 workspace, zeroed once."""
     _step_arrays(layout, plan, partials=(partials, layout.partials), out=(out, 2))
     _chk(_lib.co3_grad_norm(C.byref(layout), _dp(plan, torch.uint8), grad_scale, max_norm, _dp(out, torch.float32),
                             _dp(partials, torch.float64), _stream(stream)), "co3_grad_norm")
@@ -553,6 +556,13 @@ def step_begin(args: AdamwArgs, state, partials=None, count: Optional[int] = Non
     n = 0 if partials is None else partials.numel() if count is None else count
     _chk(_lib.co3_step_begin(C.byref(args), _dp(partials, torch.float64), n, _dp(lr, torch.float32), _dp(state, torch.uint8),
                              _stream(stream)), "co3_step_begin")
+
+
+def step_begin_norm(layout: StepLayout, plan, args: AdamwArgs, state, partials, lr=None, stream=None):
+    """The same with the norm of the gradients of a plan, in one launch; partials: float64 workspace, zeroed once."""
+    _step_arrays(layout, plan, partials=(partials, layout.partials), state=(state, STEP_STATE_BYTES))
+    _chk(_lib.co3_step_begin_norm(C.byref(layout), _dp(plan, torch.uint8), C.byref(args), _dp(partials, torch.float64),
+                                  _dp(lr, torch.float32), _dp(state, torch.uint8), _stream(stream)), "co3_step_begin_norm")
 
 
 def adamw(layout: StepLayout, plan, m, v, args: AdamwArgs, state=None, master=None, stream=None):

@@ -615,12 +615,19 @@ static bool type_ok(int32_t type) { return type == CO3_F32 || type == CO3_BF16 |
 // not negative and finite
 static bool factor_ok(double x) { return x >= 0.0 && x - x == 0.0; }
 
-// Elements of a tensor that one workgroup takes.  A workgroup of 256 lanes with four elements each has 1024 in
-// flight; one such piece per workgroup spreads a small model over the most compute units, longer ones save
-// table entries and starts.
-static int32_t step_chunk(int64_t total) { return total <= ((int64_t)1 << 22) ? 1024 : 4096; }
+// Places that a piece spans: what a workgroup of 256 lanes takes with 8 elements to a lane.  A norm gives a piece to a wavefront: 1024
+// elements are all that it has in flight at once; long gradients take four times that, to read fewer entries.
+static int32_t step_chunk(int32_t state_bits, int64_t total)
+{
+    return state_bits != 0 ? 2048 : total <= ((int64_t)1 << 22) ? 1024 : 4096;
+}
 
-#define CO3_STEP_PARTIALS_MAX 1024
+// Pieces end at places that are multiples of their length, wherever the tensor begins, so that accesses to the state arrays (and
+// to gradients that are packed as they are) are aligned behind a tensor's first piece.
+static int64_t pieces_of(int64_t place, int64_t n, int64_t chunk)
+{
+    return n == 0 ? 0 : (place + n - 1) / chunk - place / chunk + 1;
+}
 
 int32_t co3_step_layout_of(const co3_step_tensor *tensors, int32_t T, int32_t param_type, int32_t grad_type, int32_t state_bits,
                            co3_step_layout *out)
@@ -639,15 +646,19 @@ int32_t co3_step_layout_of(const co3_step_tensor *tensors, int32_t T, int32_t pa
         elems += (x.n + unit - 1) / unit * unit;
         if (elems > CO3_STEP_MAX_ELEMS) return CO3_EINVAL;
     }
-    const int32_t chunk = step_chunk(total);
-    int64_t chunks = 0;
-    for (int32_t k = 0; k < T; ++k) chunks += (tensors[k].n + chunk - 1) / chunk;
+    const int32_t chunk = step_chunk(state_bits, total);
+    int64_t chunks = 0, place = 0;
+    for (int32_t k = 0; k < T; ++k) {
+        chunks += pieces_of(place, tensors[k].n, chunk);
+        place += (tensors[k].n + unit - 1) / unit * unit;
+    }
     *out = co3_step_layout{};
     out->elems = elems;
     out->blocks = state_bits == 8 ? elems / CO3_STEP_BLOCK : 0;
     out->chunks = chunks;
     out->plan_bytes = chunks > 0 ? chunks * CO3_STEP_CHUNK_BYTES : 16;
-    out->partials = chunks < 1 ? 1 : chunks < CO3_STEP_PARTIALS_MAX ? chunks : CO3_STEP_PARTIALS_MAX;
+    const int64_t groups = (chunks + ST_NORM_WAVES - 1) / ST_NORM_WAVES;
+    out->partials = 1 + (groups < 1 ? 1 : groups < ST_NORM_GROUPS_MAX ? groups : ST_NORM_GROUPS_MAX);
     out->param_type = param_type;
     out->grad_type = grad_type;
     out->state_bits = state_bits;
@@ -703,11 +714,12 @@ int32_t co3_step_plan(const co3_step_tensor *tensors, int32_t T, const co3_step_
     int64_t place = 0;
     for (int32_t k = 0; k < T; ++k) {
         const co3_step_tensor &x = tensors[k];
-        for (int64_t i = 0; i < x.n; i += own.chunk, ++c) {
+        for (int64_t i = 0, end; i < x.n; i = end, ++c) {
+            end = std::min((place + i) / own.chunk * own.chunk + own.chunk - place, x.n);
             c->param = pb ? static_cast<char *>(x.param) + (size_t)i * pb : nullptr;
             c->grad = static_cast<const char *>(x.grad) + (size_t)i * gb;
             c->state = place + i;
-            c->count = (int32_t)std::min<int64_t>(own.chunk, x.n - i);
+            c->count = (int32_t)(end - i);
             c->lr_scale = x.lr_scale;
             c->weight_decay = x.weight_decay;
             c->reserved = 0;
@@ -720,7 +732,7 @@ int32_t co3_step_plan(const co3_step_tensor *tensors, int32_t T, const co3_step_
 static bool layout_ok(const co3_step_layout *L, const void *plan)
 {
     return L && plan && aligned(plan, 8) && L->chunks >= 0 && L->chunks <= CO3_STEP_MAX_ELEMS && L->elems >= 0 &&
-           L->elems <= CO3_STEP_MAX_ELEMS && L->partials >= 1 && L->partials <= CO3_STEP_PARTIALS_MAX && type_ok(L->grad_type) &&
+           L->elems <= CO3_STEP_MAX_ELEMS && L->partials >= 2 && L->partials <= 1 + ST_NORM_GROUPS_MAX && type_ok(L->grad_type) &&
            (L->state_bits == 0 || ((L->state_bits == 8 || L->state_bits == 32) && type_ok(L->param_type)));
 }
 
@@ -732,31 +744,46 @@ static bool norm_args_ok(double grad_scale, double max_norm)
 static bool adamw_args_ok(const co3_adamw_args *a)
 {
     return a && factor_ok(a->lr) && a->beta1 >= 0.0 && a->beta1 < 1.0 && a->beta2 >= 0.0 && a->beta2 < 1.0 && factor_ok(a->eps) &&
-           (float)a->eps > 0.0f && norm_args_ok(a->grad_scale, a->max_norm);
+           (float)a->eps >= 1.17549435e-38f && norm_args_ok(a->grad_scale, a->max_norm);
 }
 
 int32_t co3_grad_sumsq(const co3_step_layout *layout, const void *plan, double *partials, void *stream)
 {
     if (!layout_ok(layout, plan) || !partials || !aligned(partials, 8)) return CO3_EINVAL;
-    return hip_rc(co3_launch_grad_sumsq(layout, plan, partials, static_cast<hipStream_t>(stream)));
+    return hip_rc(co3_launch_grad_sumsq(layout, plan, partials, Co3StepFinish{}, static_cast<hipStream_t>(stream)));
 }
 
 int32_t co3_grad_norm(const co3_step_layout *layout, const void *plan, double grad_scale, double max_norm, float *out,
                       double *partials, void *stream)
 {
+    if (!layout_ok(layout, plan) || !partials || !aligned(partials, 8)) return CO3_EINVAL;
     if (!out || !aligned(out, 4) || !norm_args_ok(grad_scale, max_norm)) return CO3_EINVAL;
-    const int32_t rc = co3_grad_sumsq(layout, plan, partials, stream);
-    if (rc != CO3_OK) return rc;
-    return hip_rc(co3_launch_norm_finish(partials, layout->chunks ? layout->partials : 0, grad_scale, max_norm, out,
-                                         static_cast<hipStream_t>(stream)));
+    Co3StepFinish f{};
+    f.out = out;
+    f.args.grad_scale = grad_scale;
+    f.args.max_norm = max_norm;
+    return hip_rc(co3_launch_grad_sumsq(layout, plan, partials, f, static_cast<hipStream_t>(stream)));
+}
+
+static bool begin_ok(const co3_adamw_args *args, const float *lr_dev, const co3_step_state *state)
+{
+    return adamw_args_ok(args) && state && aligned(state, 8) && (!lr_dev || aligned(lr_dev, 4));
 }
 
 int32_t co3_step_begin(const co3_adamw_args *args, const double *partials, int64_t count, const float *lr_dev,
                        co3_step_state *state, void *stream)
 {
-    if (!adamw_args_ok(args) || !state || !aligned(state, 8) || count < 0 || (partials && !aligned(partials, 8))) return CO3_EINVAL;
-    if (lr_dev && !aligned(lr_dev, 4)) return CO3_EINVAL;
-    return hip_rc(co3_launch_step_begin(partials, count, args, lr_dev, state, static_cast<hipStream_t>(stream)));
+    if (!begin_ok(args, lr_dev, state) || count < 0 || (partials && !aligned(partials, 8))) return CO3_EINVAL;
+    const Co3StepFinish f{nullptr, reinterpret_cast<Co3StepDev *>(state), lr_dev, *args};
+    return hip_rc(co3_launch_step_begin(partials, count, f, static_cast<hipStream_t>(stream)));
+}
+
+int32_t co3_step_begin_norm(const co3_step_layout *layout, const void *plan, const co3_adamw_args *args, double *partials,
+                            const float *lr_dev, co3_step_state *state, void *stream)
+{
+    if (!layout_ok(layout, plan) || !partials || !aligned(partials, 8) || !begin_ok(args, lr_dev, state)) return CO3_EINVAL;
+    const Co3StepFinish f{nullptr, reinterpret_cast<Co3StepDev *>(state), lr_dev, *args};
+    return hip_rc(co3_launch_grad_sumsq(layout, plan, partials, f, static_cast<hipStream_t>(stream)));
 }
 
 static int32_t adamw_common(const co3_step_layout *layout, const void *plan, int32_t state_bits, float *master, void *m,

@@ -5,6 +5,10 @@
 
 #include "../../include/co3.h"
 
+// A norm: wavefronts of a workgroup, and the most workgroups (one to a compute unit).
+#define ST_NORM_WAVES 16
+#define ST_NORM_GROUPS_MAX 256
+
 // One piece of a tensor, at most co3_step_layout.chunk elements: what a workgroup has to know, in one entry.
 struct Co3StepChunk {
     void *param;            // first element of the piece
@@ -67,6 +71,14 @@ __host__ __device__ static inline Co3StepVar co3_step_var(const co3_adamw_args &
     return v;
 }
 
+// What is to be made of the partial sums of a norm: {norm, factor} at out, the beginning of a step at dev, or nothing.
+struct Co3StepFinish {
+    float *out;
+    Co3StepDev *dev;
+    const float *lr_dev;
+    co3_adamw_args args;
+};
+
 struct Co3StepLaunch {
     const co3_step_layout *layout;
     const void *plan;
@@ -79,9 +91,6 @@ struct Co3StepLaunch {
     const void *state;      // co3_step_state, or NULL: var and factor count
 };
 
-hipError_t co3_launch_grad_sumsq(const co3_step_layout *L, const void *plan, double *partials, hipStream_t st);
-hipError_t co3_launch_norm_finish(const double *partials, int64_t count, double grad_scale, double max_norm, float *out,
-                                  hipStream_t st);
-hipError_t co3_launch_step_begin(const double *partials, int64_t count, const co3_adamw_args *a, const float *lr_dev, void *state,
-                                 hipStream_t st);
+hipError_t co3_launch_grad_sumsq(const co3_step_layout *L, const void *plan, double *partials, const Co3StepFinish &f, hipStream_t st);
+hipError_t co3_launch_step_begin(const double *partials, int64_t count, const Co3StepFinish &f, hipStream_t st);
 hipError_t co3_launch_adamw(const Co3StepLaunch &s, hipStream_t st);

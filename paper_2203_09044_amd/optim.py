@@ -8,6 +8,7 @@ current stream of the tensors' device and return without waiting.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 from typing import List, Optional, Sequence, Union
 
@@ -16,6 +17,9 @@ import torch
 from . import binding as B
 
 PerTensor = Union[float, Sequence[float]]
+
+# the handle of a device's current stream without the object around it (0.1 us against 1.8)
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _per_tensor(x: PerTensor, T: int, what: str) -> List[float]:
@@ -49,31 +53,39 @@ class _Table:
     def __init__(self, params: Optional[Sequence[torch.Tensor]], grads: Sequence[torch.Tensor], state_bits: int,
                  lr_scales: PerTensor = 1.0, weight_decays: PerTensor = 0.0):
         self.params = None if params is None else list(params)
-        if self.params is not None:
-            _check_tensors(self.params, "parameters")
         self.state_bits = state_bits
         self._take(grads)
         T = len(self.grads)
         self.device = self.grads[0].device
         self.lr_scales, self.weight_decays = _per_tensor(lr_scales, T, "lr_scales"), _per_tensor(weight_decays, T, "weight_decay")
         self._captured = []                      # plans that a captured graph goes on reading
+        self.also = []                           # memory of the handle that its launches use
         self._make()
 
     def _take(self, grads: Sequence[torch.Tensor]):
         grads = list(grads)
-        _check_tensors(grads, "gradients")
-        like = self.params if self.params is not None else getattr(self, "grads", None)
-        if like is not None and (len(like) != len(grads) or any(p.numel() != g.numel() for p, g in zip(like, grads))):
-            raise ValueError("gradients: one per parameter, with as many elements")
-        if like is not None and grads[0].device != like[0].device:
-            raise ValueError("gradients: on the parameters' device")
+        self._check(grads)
+        self.sizes = [g.numel() for g in grads]
         self.grads = grads
+        self._where = [t.data_ptr for t in self.grads + (self.params or [])]
+
+    def _check(self, grads: Sequence[torch.Tensor]):
+        _check_tensors(grads, "gradients")
+        sizes = getattr(self, "sizes", None) or [p.numel() for p in self.params or grads]
+        if self.params is not None:
+            _check_tensors(self.params, "parameters")
+            if sizes != [p.numel() for p in self.params]:
+                raise ValueError("parameters: as many elements as before")
+            if grads[0].device != self.params[0].device:
+                raise ValueError("gradients: on the parameters' device")
+        if sizes != [g.numel() for g in grads]:
+            raise ValueError("gradients: one per parameter, with as many elements")
 
     def _addresses(self) -> List[int]:
-        a = [g.data_ptr() for g in self.grads]
-        return a if self.params is None else a + [p.data_ptr() for p in self.params]
+        return [f() for f in self._where]
 
     def _make(self):
+        self._check(self.grads)
         self._at = self._addresses()
         T = len(self.grads)
         rows = (B.StepTensor * T)()
@@ -89,38 +101,47 @@ class _Table:
             raise ValueError("a parameter shares memory with another one or with a gradient") from e
         with torch.cuda.device(self.device):
             self.plan = host.to(self.device)
-            self._home = torch.cuda.current_stream(self.device).cuda_stream
+            self._streams = {_raw_stream(self.device.index)}     # streams that the memory is known to
         self.plan_ptr = C.c_void_p(self.plan.data_ptr())
 
-    def ready(self, grads: Optional[Sequence[torch.Tensor]]) -> int:
-        """The plan is that of the tensors as they lie now; returns the raw current stream of their device."""
+    def ready(self, grads: Optional[Sequence[torch.Tensor]], capturable: bool = True) -> C.c_void_p:
+        """The plan is that of the tensors as they lie now; returns the current stream of their device, which is the current one."""
         if grads is not None:
             was = self.grads[0].dtype
             self._take(grads)
             if self.grads[0].dtype != was:
                 self._at = None
         capturing = torch.cuda.is_current_stream_capturing()
+        if capturing and not capturable:
+            raise RuntimeError("a captured step needs device_steps=True")
         if self._at != self._addresses():
             if capturing:
-                raise RuntimeError("a tensor has moved since the last step: step once before the capture")
+                raise RuntimeError("a tensor has moved since the last call: call once before the capture")
             self._make()
-        stream = torch.cuda.current_stream(self.device)
-        raw = stream.cuda_stream
-        if capturing and not any(p is self.plan for p in self._captured):
-            self._captured.append(self.plan)
-        elif raw != self._home:
-            self.plan.record_stream(stream)
-        return raw
+        raw = _raw_stream(self.device.index)
+        if capturing:
+            if not any(p is self.plan for p in self._captured):
+                self._captured.append(self.plan)
+        elif raw not in self._streams:
+            self._streams.add(raw)
+            for t in [self.plan] + self.also:
+                t.record_stream(torch.cuda.current_stream(self.device))
+        return C.c_void_p(raw)
 
 
-class _OnDevice:
+def _on_device(call):
     """Launches of a handle go to its tensors' device, whichever is current."""
+    @functools.wraps(call)
+    def there(self, grads=None):
+        device = self._table.device
+        if torch.cuda.current_device() == device.index:
+            return call(self, grads)
+        with torch.cuda.device(device):
+            return call(self, grads)
+    return there
 
-    def _guard(self):
-        return torch.cuda.device(self._table.device)
 
-
-class GradNorm(_OnDevice):
+class GradNorm:
     """Global L2 norm of gradients that lie in many tensors, with the factor that clips it.
 
     ``compute()`` returns a float32 tensor of two on the device, (norm, factor): norm = grad_scale * sqrt(sum g^2),
@@ -134,20 +155,21 @@ class GradNorm(_OnDevice):
         self._table = _Table(None, grads, 0)
         dev = self._table.device
         self._out = torch.zeros(2, dtype=torch.float32, device=dev)
-        self._partials = torch.empty(self._table.layout.partials, dtype=torch.float64, device=dev)
+        self._partials = torch.zeros(self._table.layout.partials, dtype=torch.float64, device=dev)
         self._ptrs = C.c_void_p(self._out.data_ptr()), C.c_void_p(self._partials.data_ptr())
+        self._table.also = [self._out, self._partials]
+        torch.cuda.current_stream(dev).synchronize()       # cleared, for whichever stream comes first
 
+    @_on_device
     def compute(self, grads: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
         """``grads``: None, or tensors of the same sizes to take instead, from now on."""
         t = self._table
-        with self._guard():
-            raw = t.ready(grads)
-            B._chk(B._lib.co3_grad_norm(t.layout_ref, t.plan_ptr, self.grad_scale, self.max_norm, self._ptrs[0], self._ptrs[1],
-                                        C.c_void_p(raw)), "co3_grad_norm")
+        stream = t.ready(grads)
+        B._chk(B._lib.co3_grad_norm(t.layout_ref, t.plan_ptr, self.grad_scale, self.max_norm, *self._ptrs, stream), "co3_grad_norm")
         return self._out
 
 
-class AdamW(_OnDevice):
+class AdamW:
     """AdamW over many tensors at once (the formulas: ``include/co3.h``).
 
     params, grads   tensors of one type each (float32, bfloat16, float16), contiguous, on one device; written and read in place
@@ -172,8 +194,8 @@ class AdamW(_OnDevice):
             raise ValueError("state_bits must be 8 or 32")
         if not all(0.0 <= b < 1.0 for b in betas):
             raise ValueError("betas must be in [0, 1)")
-        if not (C.c_float(eps).value > 0.0 and math.isfinite(eps)):
-            raise ValueError("eps must be positive, in float32 too")
+        if not (C.c_float(eps).value >= 2.0 ** -126 and math.isfinite(eps)):
+            raise ValueError("eps must be finite and at least 2^-126")
         if max_norm is not None and not max_norm > 0.0:
             raise ValueError("max_norm must be positive")
         if not (grad_scale > 0.0 and math.isfinite(grad_scale)):
@@ -206,9 +228,12 @@ class AdamW(_OnDevice):
         self._dev = torch.zeros(B.STEP_STATE_BYTES // 8, dtype=torch.int64, **z)
         self._dev_ptr = C.c_void_p(self._dev.data_ptr())
         self.norm = self._dev.view(torch.float32)[4:6]        # (norm, factor) of the last step that took a norm
-        self._partials = torch.empty(t.layout.partials if max_norm is not None else 1, dtype=torch.float64, **z)
+        self._partials = torch.zeros(t.layout.partials if max_norm is not None else 1, dtype=torch.float64, **z)
+        self._partials_ptr = C.c_void_p(self._partials.data_ptr())
         self._device_steps = device_steps or max_norm is not None
         self.lr = lr
+        t.also = [self._dev, self._partials, *self._named().values()]
+        torch.cuda.current_stream(t.device).synchronize()      # cleared, for whichever stream comes first
 
     # ---- what a program sets and reads
     @property
@@ -220,24 +245,22 @@ class AdamW(_OnDevice):
         if isinstance(lr, torch.Tensor):
             if lr.dtype != torch.float32 or lr.numel() != 1 or lr.device != self._table.device:
                 raise ValueError("lr: a float32 tensor of one element on the parameters' device")
-            if not self._on_device:
+            if not self._device_steps:              # the device counts from here on
                 self._dev[0] = self._t
                 self._device_steps = True
             self._args.lr = 0.0
+            self._lr_ptr = C.c_void_p(lr.data_ptr())
         elif not (lr >= 0.0 and math.isfinite(lr)):
             raise ValueError("lr must be finite and not negative")
         else:
             self._args.lr = float(lr)
+            self._lr_ptr = None
         self._lr = lr
-
-    @property
-    def _on_device(self) -> bool:
-        return self._device_steps
 
     @property
     def t(self) -> int:
         """Number of steps taken (waits for the device where that counts them)."""
-        return int(self._dev[0].item()) if self._on_device else self._t
+        return int(self._dev[0].item()) if self._device_steps else self._t
 
     @t.setter
     def t(self, t: int):
@@ -295,25 +318,22 @@ class AdamW(_OnDevice):
         self._dev[1] = d["skipped"]
 
     # ---- the step
+    @_on_device
     def step(self, grads: Optional[Sequence[torch.Tensor]] = None):
         """One step on every tensor.  ``grads``: None, or tensors of the same sizes to take instead, from now on."""
         t = self._table
-        with self._guard():
-            raw = t.ready(grads)
-            stream = C.c_void_p(raw)
-            state = None
-            if self._on_device:
-                state, partials, count = self._dev_ptr, None, 0
-                if self.max_norm is not None:
-                    partials, count = C.c_void_p(self._partials.data_ptr()), t.layout.partials if t.layout.chunks else 0
-                    B._chk(B._lib.co3_grad_sumsq(t.layout_ref, t.plan_ptr, partials, stream), "co3_grad_sumsq")
-                lr = C.c_void_p(self._lr.data_ptr()) if isinstance(self._lr, torch.Tensor) else None
-                B._chk(B._lib.co3_step_begin(self._args_ref, partials, count, lr, state, stream), "co3_step_begin")
+        stream = t.ready(grads, self._device_steps)
+        state = None
+        if self._device_steps:
+            state = self._dev_ptr
+            if self.max_norm is not None:
+                B._chk(B._lib.co3_step_begin_norm(t.layout_ref, t.plan_ptr, self._args_ref, self._partials_ptr, self._lr_ptr, state, stream),
+                       "co3_step_begin_norm")
             else:
-                if torch.cuda.is_current_stream_capturing():
-                    raise RuntimeError("a captured step needs device_steps=True")
-                self._args.t = self._t + 1
-            B._chk(self._step_fn(t.layout_ref, t.plan_ptr, self._master_ptr, *self._state_ptrs, self._args_ref, state, stream),
-                   "co3_adamw" if self.state_bits == 32 else "co3_adamw8")
-            if state is None:
-                self._t += 1
+                B._chk(B._lib.co3_step_begin(self._args_ref, None, 0, self._lr_ptr, state, stream), "co3_step_begin")
+        else:
+            self._args.t = self._t + 1
+        B._chk(self._step_fn(t.layout_ref, t.plan_ptr, self._master_ptr, *self._state_ptrs, self._args_ref, state, stream),
+               "co3_adamw" if self.state_bits == 32 else "co3_adamw8")
+        if state is None:
+            self._t += 1

@@ -123,16 +123,18 @@ def test_plan_covers_every_element_once(B, bits, pt, gt, sizes):
     unit = 256 if bits == 8 else 1
     starts = np.concatenate([[0], np.cumsum([-(-n // unit) * unit for n in sizes])])
     assert L.elems == starts[-1] and L.blocks == (L.elems // 256 if bits == 8 else 0)
-    assert L.chunks == sum(-(-n // L.chunk) for n in sizes) and L.chunk % 256 == 0 and L.partials >= 1
+    assert L.chunk % 256 == 0 and L.partials >= 2
     plan = B.step_plan(t, L).numpy()
     assert plan.nbytes == L.plan_bytes
     entries = plan[:L.chunks * 40].view(np.dtype([("p", "<u8"), ("g", "<u8"), ("at", "<i8"), ("n", "<i4"), ("ls", "<f4"), ("wd", "<f4"), ("x", "<i4")]))
     k = 0
     for n, x, at in zip(sizes, t, starts):
-        for i in range(0, n, L.chunk):
+        i = 0
+        while i < n:                                # a piece ends at a multiple of its length, or with its tensor
             e = entries[k]
-            assert e["g"] == x.grad + i * gb and e["at"] == at + i and e["n"] == min(L.chunk, n - i)
+            assert e["g"] == x.grad + i * gb and e["at"] == at + i and e["n"] == min(L.chunk - (at + i) % L.chunk, n - i)
             assert e["p"] == (x.param + i * pb if bits else 0)
+            i += int(e["n"])
             k += 1
     assert k == len(entries)
 
@@ -188,13 +190,14 @@ def test_device_calls_refuse_bad_arguments_on_the_host(B):
     good = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, max_norm=1.0, t=1, seed=0)
     args = lambda **kw: C.byref(B.AdamwArgs(**{**good, **kw}))  # noqa: E731
     bad = [dict(lr=-1.0), dict(lr=math.nan), dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=math.nan),
-           dict(eps=0.0), dict(eps=1e-60), dict(eps=math.nan), dict(grad_scale=0.0), dict(grad_scale=math.inf), dict(grad_scale=-1.0),
+           dict(eps=0.0), dict(eps=1e-60), dict(eps=1e-39), dict(eps=math.nan), dict(grad_scale=0.0), dict(grad_scale=math.inf), dict(grad_scale=-1.0),
            dict(max_norm=0.0), dict(max_norm=math.nan), dict(t=0)]
     for kw in bad:
         assert lib.co3_adamw(C.byref(L32), p, None, p, p, args(**kw), None, None) == B.EINVAL, kw
         assert lib.co3_adamw8(C.byref(L8), p, None, p, p, p, p, args(**kw), None, None) == B.EINVAL, kw
         if "t" not in kw:
             assert lib.co3_step_begin(args(**kw), None, 0, None, p, None) == B.EINVAL, kw
+            assert lib.co3_step_begin_norm(C.byref(L32), p, args(**kw), p, None, p, None) == B.EINVAL, kw
     for a in ((None, p, None, p, p), (C.byref(L32), None, None, p, p), (C.byref(L8), p, None, p, p), (C.byref(L0), p, None, p, p),
               (C.byref(L32), p, p, p, p), (C.byref(L32), p, None, None, p), (C.byref(L32), p, None, p, None),
               (C.byref(L32), p, None, odd, p), (C.byref(L32), odd, None, p, p)):
@@ -208,6 +211,10 @@ def test_device_calls_refuse_bad_arguments_on_the_host(B):
               (C.byref(L0), p, 1.0, 0.0, p, p), (C.byref(L0), p, math.nan, 1.0, p, p), (C.byref(L0), p, 1.0, math.nan, p, p),
               (None, p, 1.0, 1.0, p, p), (C.byref(L0), None, 1.0, 1.0, p, p), (C.byref(L0), p, 1.0, 1.0, p, odd)):
         assert lib.co3_grad_norm(*a, None) == B.EINVAL
+    for a in ((None, p, args(), p, None, p), (C.byref(L32), None, args(), p, None, p), (C.byref(L32), p, None, p, None, p),
+              (C.byref(L32), p, args(), None, None, p), (C.byref(L32), p, args(), odd, None, p), (C.byref(L32), p, args(), p, odd, p),
+              (C.byref(L32), p, args(), p, None, None), (C.byref(L32), p, args(), p, None, odd)):
+        assert lib.co3_step_begin_norm(*a, None) == B.EINVAL
     assert lib.co3_grad_sumsq(C.byref(L0), p, None, None) == B.EINVAL
     for a in ((args(), None, 0, None, None), (args(), None, -1, None, p), (args(), odd, 1, None, p), (args(), None, 0, odd, p),
               (args(), None, 0, None, odd), (None, None, 0, None, p)):
