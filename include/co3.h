@@ -455,7 +455,7 @@ typedef struct {
 
 typedef struct {
     double lr, beta1, beta2, eps; /* lr >= 0, 0 <= beta < 1, eps >= 2^-126 in fp32 */
-    double grad_scale;            /* multiplies every gradient, > 0 (1: as they are) */
+    double grad_scale;            /* multiplies every gradient, 2^-126 .. 2^127 (1: as they are) */
     double max_norm;              /* > 0; the norm beyond which gradients are scaled down (INFINITY: never) */
     int64_t t;                    /* number of this step, from 1; used where no co3_step_state is given */
     uint64_t seed;                /* of the rounding of 8-bit states */
@@ -471,7 +471,7 @@ typedef struct {
 } co3_step_state;
 
 /* Sizes for T >= 1 tensors.  Host only.  CO3_EINVAL: a null or misaligned address, a negative or too large size (elems
- * <= 2^33), a factor that is negative or not finite, types or state_bits other than the above. */
+ * <= 2^33, chunks <= 2^23), a factor that is negative or not finite, types or state_bits other than the above. */
 int32_t co3_step_layout_of(const co3_step_tensor *tensors_host, int32_t T, int32_t param_type, int32_t grad_type,
                            int32_t state_bits, co3_step_layout *layout_host);
 

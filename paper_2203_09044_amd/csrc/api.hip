@@ -622,6 +622,8 @@ static int32_t step_chunk(int32_t state_bits, int64_t total)
     return state_bits != 0 ? 2048 : total <= ((int64_t)1 << 22) ? 1024 : 4096;
 }
 
+#define CO3_STEP_MAX_CHUNKS ((int64_t)1 << 23)     // of 256 lanes each, a grid below 2^32
+
 // Pieces end at places that are multiples of their length, wherever the tensor begins, so that accesses to the state arrays (and
 // to gradients that are packed as they are) are aligned behind a tensor's first piece.
 static int64_t pieces_of(int64_t place, int64_t n, int64_t chunk)
@@ -652,6 +654,7 @@ int32_t co3_step_layout_of(const co3_step_tensor *tensors, int32_t T, int32_t pa
         chunks += pieces_of(place, tensors[k].n, chunk);
         place += (tensors[k].n + unit - 1) / unit * unit;
     }
+    if (chunks > CO3_STEP_MAX_CHUNKS) return CO3_EINVAL;
     *out = co3_step_layout{};
     out->elems = elems;
     out->blocks = state_bits == 8 ? elems / CO3_STEP_BLOCK : 0;
@@ -731,14 +734,14 @@ int32_t co3_step_plan(const co3_step_tensor *tensors, int32_t T, const co3_step_
 
 static bool layout_ok(const co3_step_layout *L, const void *plan)
 {
-    return L && plan && aligned(plan, 8) && L->chunks >= 0 && L->chunks <= CO3_STEP_MAX_ELEMS && L->elems >= 0 &&
+    return L && plan && aligned(plan, 8) && L->chunks >= 0 && L->chunks <= CO3_STEP_MAX_CHUNKS && L->elems >= 0 &&
            L->elems <= CO3_STEP_MAX_ELEMS && L->partials >= 2 && L->partials <= 1 + ST_NORM_GROUPS_MAX && type_ok(L->grad_type) &&
            (L->state_bits == 0 || ((L->state_bits == 8 || L->state_bits == 32) && type_ok(L->param_type)));
 }
 
 static bool norm_args_ok(double grad_scale, double max_norm)
 {
-    return grad_scale > 0.0 && factor_ok(grad_scale) && max_norm > 0.0;
+    return grad_scale >= 1.17549435e-38 && grad_scale <= 3.4028234e38 && max_norm > 0.0;
 }
 
 static bool adamw_args_ok(const co3_adamw_args *a)

@@ -202,13 +202,11 @@ __global__ __launch_bounds__(ST_NORM_BLOCK) void k_grad_sumsq(const Co3StepChunk
         return;
     }
     if (threadIdx.x == 0) {
-        uint32_t *next = reinterpret_cast<uint32_t *>(partials + gridDim.x);
-        // The sum is written through to where every compute unit sees it, and has arrived there before the ticket is taken; a
-        // release would write back the whole of the L2 first (2048 of them: 78 us).
+        // The sum is written through to where every compute unit sees it, and has arrived there before the ticket is drawn; a
+        // release would write back the whole of the L2 first (2048 of them: 78 us).  The last ticket sets the counter back.
         __hip_atomic_store(partials + blockIdx.x, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        ticket = __hip_atomic_fetch_add(next, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (ticket == gridDim.x - 1) __hip_atomic_store(next, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        ticket = atomicInc(reinterpret_cast<uint32_t *>(partials + gridDim.x), gridDim.x - 1);
     }
     __syncthreads();
     if (ticket != gridDim.x - 1) return;

@@ -31,6 +31,11 @@ def _per_tensor(x: PerTensor, T: int, what: str) -> List[float]:
     return values
 
 
+def _check_scale(grad_scale: float):
+    if not 2.0 ** -126 <= grad_scale <= 2.0 ** 127:
+        raise ValueError("grad_scale must be between 2^-126 and 2^127")
+
+
 def _check_tensors(tensors: Sequence[torch.Tensor], what: str):
     if not tensors:
         raise ValueError(f"no {what}")
@@ -149,8 +154,9 @@ class GradNorm:
     next call overwrites it."""
 
     def __init__(self, grads: Sequence[torch.Tensor], max_norm: float = math.inf, grad_scale: float = 1.0):
-        if not max_norm > 0.0 or not (grad_scale > 0.0 and math.isfinite(grad_scale)):
-            raise ValueError("max_norm and grad_scale must be positive, grad_scale finite")
+        if not max_norm > 0.0:
+            raise ValueError("max_norm must be positive")
+        _check_scale(grad_scale)
         self.max_norm, self.grad_scale = float(max_norm), float(grad_scale)
         self._table = _Table(None, grads, 0)
         dev = self._table.device
@@ -198,8 +204,7 @@ class AdamW:
             raise ValueError("eps must be finite and at least 2^-126")
         if max_norm is not None and not max_norm > 0.0:
             raise ValueError("max_norm must be positive")
-        if not (grad_scale > 0.0 and math.isfinite(grad_scale)):
-            raise ValueError("grad_scale must be positive and finite")
+        _check_scale(grad_scale)
         self._table = t = _Table(params, grads, state_bits, lr_scales, weight_decay)
         if master and t.params[0].dtype == torch.float32:
             raise ValueError("float32 parameters are their own masters")
@@ -337,3 +342,4 @@ class AdamW:
                "co3_adamw" if self.state_bits == 32 else "co3_adamw8")
         if state is None:
             self._t += 1
+        torch.autograd.graph.increment_version(t.params)       # written in place, though not by torch

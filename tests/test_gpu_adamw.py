@@ -264,6 +264,25 @@ def test_norm(co3, dtype, sizes, skew):
         assert abs(out[0] - norm) <= U * (1 + 1e-6) * norm and abs(out[1] - c) <= U * (1 + 1e-6) * c
 
 
+@pytest.mark.parametrize("dtype,n", [(F32, 40_000_003), (BF16, 100_000_001), (F16, 70_000_007)])
+def test_norm_of_gradients_beyond_the_caches(co3, dtype, n):
+    g = torch.empty(n + 1, dtype=dtype, device="cuda").normal_(std=0.01)[1:]
+    for _ in range(3):
+        out = co3.GradNorm([g[:n // 3], g[n // 3:]], max_norm=1.0).compute().tolist()
+        norm = float(torch.linalg.vector_norm(g.double()))
+        assert abs(out[0] - norm) <= U * (1 + 1e-6) * norm and abs(out[1] - 1 / (norm + 1e-6)) <= U * (1 + 1e-6) / norm
+        g.mul_(1.5)
+
+
+def test_autograd_sees_that_the_parameters_changed(co3):
+    p = torch.nn.Parameter(torch.randn(100, device="cuda"))
+    opt = co3.AdamW([p], [torch.ones(100, device="cuda")])
+    y = (p * p).sum()
+    opt.step()
+    with pytest.raises(RuntimeError):
+        y.backward()
+
+
 def test_norm_at_the_ends_of_the_range(co3):
     big = torch.full((1000,), 3e38, device="cuda")
     out = co3.GradNorm([big], max_norm=1.0).compute()

@@ -190,7 +190,7 @@ def test_device_calls_refuse_bad_arguments_on_the_host(B):
     good = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, max_norm=1.0, t=1, seed=0)
     args = lambda **kw: C.byref(B.AdamwArgs(**{**good, **kw}))  # noqa: E731
     bad = [dict(lr=-1.0), dict(lr=math.nan), dict(lr=math.inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=math.nan),
-           dict(eps=0.0), dict(eps=1e-60), dict(eps=1e-39), dict(eps=math.nan), dict(grad_scale=0.0), dict(grad_scale=math.inf), dict(grad_scale=-1.0),
+           dict(eps=0.0), dict(eps=1e-60), dict(eps=1e-39), dict(eps=math.nan), dict(grad_scale=0.0), dict(grad_scale=math.inf), dict(grad_scale=1e-39), dict(grad_scale=1e39), dict(grad_scale=-1.0),
            dict(max_norm=0.0), dict(max_norm=math.nan), dict(t=0)]
     for kw in bad:
         assert lib.co3_adamw(C.byref(L32), p, None, p, p, args(**kw), None, None) == B.EINVAL, kw
