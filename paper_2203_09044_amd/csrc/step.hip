@@ -132,8 +132,23 @@ __device__ __forceinline__ double block_sum_f64(double s, double *red)
 }
 
 // What is made of the partial sums of a norm, by one workgroup: {norm, factor} at `out`, or the beginning of a step that the
-// device counts (a captured step has no other way to).  The factor is negative where the norm is not finite.
-__device__ __forceinline__ void finish_norm(double s, bool norm, const Co3StepFinish &f)
+// device counts (a captured step has no other way to).  The factor is negative where the norm is not finite.  What follows from the
+// number of the step alone (two powers, quotients and a root in 64 bits) is made by a wavefront that has nothing else to do
+// while the sums arrive.
+struct StepNext {
+    int64_t t;
+    Co3StepVar var;
+};
+__device__ __forceinline__ void prepare_next(const Co3StepFinish &f, StepNext *next)      // before the sum's barrier
+{
+    if (!f.dev || threadIdx.x != CO3_WAVE) return;
+    co3_adamw_args a = f.args;
+    a.t = f.dev->t + 1;
+    if (f.lr_dev) a.lr = (double)*f.lr_dev;
+    next->t = a.t;
+    next->var = co3_step_var(a);
+}
+__device__ __forceinline__ void finish_norm(double s, bool norm, const Co3StepFinish &f, const StepNext *next)     // one lane
 {
     float factor = (float)f.args.grad_scale, total32 = 0.0f;
     if (norm) {
@@ -153,11 +168,8 @@ __device__ __forceinline__ void finish_norm(double s, bool norm, const Co3StepFi
         f.dev->skipped += 1;
         return;
     }
-    co3_adamw_args a = f.args;
-    a.t = f.dev->t + 1;
-    f.dev->t = a.t;
-    if (f.lr_dev) a.lr = (double)*f.lr_dev;
-    f.dev->var = co3_step_var(a);
+    f.dev->t = next->t;
+    f.dev->var = next->var;
 }
 
 // partials[workgroup] = sum of the squares of its pieces; a wavefront takes a piece, ROUNDS vectors of it in flight.  In 64 bits: the
@@ -174,6 +186,7 @@ __global__ __launch_bounds__(ST_NORM_BLOCK) void k_grad_sumsq(const Co3StepChunk
     constexpr int V = Elems<G>::WIDE, ROUNDS = 32 / V, STEP = CO3_WAVE * V;
     __shared__ double red[ST_NORM_WAVES];
     __shared__ uint32_t ticket;
+    __shared__ StepNext next;
     const int lane = threadIdx.x & (CO3_WAVE - 1);
     double s[4] = {0.0, 0.0, 0.0, 0.0};
     for (int64_t k = (int64_t)blockIdx.x * ST_NORM_WAVES + __builtin_amdgcn_readfirstlane((int)threadIdx.x / CO3_WAVE); k < chunks;
@@ -210,23 +223,25 @@ __global__ __launch_bounds__(ST_NORM_BLOCK) void k_grad_sumsq(const Co3StepChunk
     }
     __syncthreads();
     if (ticket != gridDim.x - 1) return;
+    prepare_next(f, &next);
     double all = 0.0;
     for (uint32_t i = threadIdx.x; i < gridDim.x; i += ST_NORM_BLOCK)
         all += __hip_atomic_load(partials + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     all = block_sum_f64(all, red);
-    if (threadIdx.x == 0) finish_norm(all, true, f);
+    if (threadIdx.x == 0) finish_norm(all, true, f, &next);
 }
 
 // The same from partial sums that are there already (several tables under one norm), or without a norm.
 __global__ __launch_bounds__(ST_NORM_BLOCK) void k_step_begin(const double *__restrict__ partials, int64_t count, Co3StepFinish f)
 {
     __shared__ double red[ST_NORM_WAVES];
+    __shared__ StepNext next;
+    prepare_next(f, &next);
     double s = 0.0;
-    if (partials) {
+    if (partials)
         for (int64_t i = threadIdx.x; i < count; i += ST_NORM_BLOCK) s += partials[i];
-        s = block_sum_f64(s, red);
-    }
-    if (threadIdx.x == 0) finish_norm(s, partials != nullptr, f);
+    s = block_sum_f64(s, red);
+    if (threadIdx.x == 0) finish_norm(s, partials != nullptr, f, &next);
 }
 
 // ---- step ---------------------------------------------------------------------------------------------------
