@@ -422,7 +422,7 @@ void co3_set_exchange_spin_limit(int64_t polls);
  * that is cut off rounds the number up with its own probability: by 16 bits of a hash of (seed, t, place), the
  * complement of m's for r, so that equal calls give equal results.  (Rounding to nearest would hold r where it is: a
  * step moves v by some 1 - beta2 of itself, the next number is 12 % away.)  An r that is not zero does not become zero.
- * Where a gradient is not finite, its block's states are not either, or no longer say anything.
+ * Where a gradient or its square is not finite, the states of its block are lost.
  */
 #define CO3_F32 0
 #define CO3_BF16 1

@@ -72,6 +72,9 @@ class _Table:
         self._check(grads)
         self.sizes = [g.numel() for g in grads]
         self.grads = grads
+        self._watch()
+
+    def _watch(self):
         self._where = [t.data_ptr for t in self.grads + (self.params or [])]
 
     def _check(self, grads: Sequence[torch.Tensor]):
@@ -91,38 +94,39 @@ class _Table:
 
     def _make(self):
         self._check(self.grads)
-        self._at = self._addresses()
-        T = len(self.grads)
+        at, T = self._addresses(), len(self.grads)
         rows = (B.StepTensor * T)()
-        for k, g in enumerate(self.grads):
-            rows[k] = B.StepTensor(None if self.params is None else self._at[T + k], self._at[k], g.numel(), self.lr_scales[k],
-                                   self.weight_decays[k])
-        self.layout = B.step_layout_of(rows, B.TYPE_NONE if self.params is None else B.TYPE_OF[self.params[0].dtype],
-                                       B.TYPE_OF[self.grads[0].dtype], self.state_bits)
-        self.layout_ref = C.byref(self.layout)
+        for k, n in enumerate(self.sizes):
+            rows[k] = B.StepTensor(None if self.params is None else at[T + k], at[k], n, self.lr_scales[k], self.weight_decays[k])
+        layout = B.step_layout_of(rows, B.TYPE_NONE if self.params is None else B.TYPE_OF[self.params[0].dtype],
+                                  B.TYPE_OF[self.grads[0].dtype], self.state_bits)
         try:
-            host = B.step_plan(rows, self.layout)
+            host = B.step_plan(rows, layout)
         except B.Co3Error as e:
             raise ValueError("a parameter shares memory with another one or with a gradient") from e
         with torch.cuda.device(self.device):
             self.plan = host.to(self.device)
             self._streams = {_raw_stream(self.device.index)}     # streams that the memory is known to
-        self.plan_ptr = C.c_void_p(self.plan.data_ptr())
+        self.layout, self.layout_ref, self.plan_ptr = layout, C.byref(layout), C.c_void_p(self.plan.data_ptr())
+        self._at, self._dtype = at, self.grads[0].dtype          # what the plan is for
 
     def ready(self, grads: Optional[Sequence[torch.Tensor]], capturable: bool = True) -> C.c_void_p:
         """The plan is that of the tensors as they lie now; returns the current stream of their device, which is the current one."""
-        if grads is not None:
-            was = self.grads[0].dtype
-            self._take(grads)
-            if self.grads[0].dtype != was:
-                self._at = None
         capturing = torch.cuda.is_current_stream_capturing()
         if capturing and not capturable:
             raise RuntimeError("a captured step needs device_steps=True")
-        if self._at != self._addresses():
-            if capturing:
-                raise RuntimeError("a tensor has moved since the last call: call once before the capture")
-            self._make()
+        was = self.grads
+        if grads is not None:
+            self._take(grads)
+        if self._at != self._addresses() or self._dtype != self.grads[0].dtype:
+            try:
+                if capturing:
+                    raise RuntimeError("a tensor has moved since the last call: call once before the capture")
+                self._make()
+            except Exception:
+                self.grads = was                                 # refused gradients are not kept
+                self._watch()
+                raise
         raw = _raw_stream(self.device.index)
         if capturing:
             if not any(p is self.plan for p in self._captured):

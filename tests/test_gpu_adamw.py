@@ -415,8 +415,18 @@ def test_tensors_that_move_and_gradients_that_change(co3, bits):
         opt.step([torch.zeros(1000, device="cuda"), torch.zeros(31, device="cuda")])
     with pytest.raises(ValueError):
         opt.step([torch.zeros(1000), torch.zeros(30)])
+    with pytest.raises(ValueError):
+        opt.step([x.detach() for x in p])               # the parameters themselves
+    ref.step()
+    opt.step()                                          # what was refused is not kept: the gradients are those before
+    assert all(torch.equal(a, b.detach()) for a, b in zip(ref_p, p))
     opt.step([x.to(BF16) for x in ref._table.grads])    # of another type
-    assert opt.t == 5
+    ref.step([x.to(BF16) for x in ref._table.grads])
+    assert opt.t == ref.t == 6 and all(torch.equal(a, b.detach()) for a, b in zip(ref_p, p))
+    p[0].data = p[0].data[:999].clone()                 # another tensor than the states are for
+    with pytest.raises(ValueError):
+        opt.step()
+    assert opt.t == 6
 
 
 @pytest.mark.parametrize("bits,ptype", [(32, F32), (8, F32), (8, BF16)])
@@ -438,6 +448,42 @@ def test_a_saved_state_goes_on_as_the_run_does(co3, bits, ptype):
     assert all(torch.equal(x, y) for x, y in zip(a, b)) and opt.t == other.t == 6
     with pytest.raises(ValueError):
         co3.AdamW(b, gs[0], state_bits=40 - bits).load_state_dict(saved)
+
+
+def test_a_replay_after_its_tensors_plan_was_made_anew(co3):
+    """A captured step goes on with the memory it was captured with, whatever the handle steps later."""
+    p, g = torch.randn(5000, device="cuda"), torch.randn(5000, device="cuda")
+    opt = co3.AdamW([p], [g], device_steps=True, lr=1e-3)
+    ref_p = p.clone()
+    ref = co3.AdamW([ref_p], [g], device_steps=True, lr=1e-3)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    for t in range(3):
+        graph.replay()
+        opt.step([torch.full_like(g, 0.1 * t)])          # eager, each time from a gradient of its own
+        filler = [torch.full((4096,), float("nan"), device="cuda") for _ in range(64)]
+        ref.step([g])
+        ref.step([torch.full_like(g, 0.1 * t)])
+        torch.cuda.synchronize()
+        assert torch.equal(p, ref_p) and opt.t == ref.t == 2 * t + 2 and filler
+
+
+def test_handles_made_on_one_stream_and_used_on_another(co3):
+    side = torch.cuda.Stream()
+    torch.manual_seed(8)
+    p, g = torch.randn(3_000_000, device="cuda"), torch.randn(3_000_000, device="cuda")
+    want = p.clone()
+    co3.AdamW([want], [g], state_bits=8, max_norm=1.0).step()
+    torch.cuda.synchronize()
+    opt = co3.AdamW([p], [g], state_bits=8, max_norm=1.0)
+    with torch.cuda.stream(side):
+        opt.step()
+        norm = co3.GradNorm([g]).compute()
+    del opt                                             # its memory is not given away before the step has run
+    junk = [torch.full((1 << 20,), float("nan"), device="cuda") for _ in range(16)]
+    torch.cuda.synchronize()
+    assert torch.equal(p, want) and junk and abs(float(norm[0]) - float(torch.linalg.vector_norm(g.double()))) < 1e-3
 
 
 def test_tensors_of_no_elements(co3):
