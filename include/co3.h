@@ -446,7 +446,7 @@ typedef struct {
     int64_t elems;          /* length of the state arrays (and of the master array), in elements */
     int64_t blocks;         /* scales of each 8-bit state, 0 with 32-bit states */
     int64_t chunks;         /* entries of the plan */
-    int64_t plan_bytes;     /* bytes of the plan, at least 16 */
+    int64_t plan_bytes;     /* bytes of the plan */
     int64_t partials;       /* doubles of workspace that a norm needs */
     int32_t param_type, grad_type;
     int32_t state_bits;     /* 32, 8, or 0 for a norm alone */
@@ -462,7 +462,7 @@ typedef struct {
 } co3_adamw_args;
 
 /* Device memory of the caller, 8-byte aligned, zeroed once: what a step that the device counts goes by.  t is the number of steps
- * taken, skipped how many were left out; norm and factor are those of the last co3_step_begin.  The rest is the
+ * taken, skipped how many were left out; norm and factor are those of the last step that took a norm.  The rest is the
  * library's. */
 typedef struct {
     int64_t t, skipped;
@@ -498,16 +498,15 @@ int32_t co3_grad_norm(const co3_step_layout *layout_host, const void *plan, doub
                       double *partials, void *stream);
 
 /*
- * Begins a step that the device counts (for captured steps, clipped ones, learning rates that the device holds).
- * co3_step_begin: partials NULL (no norm is taken, the factor is grad_scale), or count doubles that calls of co3_grad_sumsq have
- * filled, from which norm and factor follow as in co3_grad_norm.  co3_step_begin_norm: the norm is that of the gradients of
- * the plan, taken in the same launch (partials: workspace).  If the norm is not finite, state->skipped goes up, and the
- * step that follows changes nothing; else state->t goes up.  lr_dev: NULL, or a device float that stands for args->lr.
+ * Begins a step that the device counts (for captured steps, learning rates that the device holds, several tables under one
+ * norm): state->t goes up, and the calls of co3_adamw and co3_adamw8 that follow on this stream are that step.
+ *   partials   NULL (no norm is taken, the factor is grad_scale), or count doubles that calls of co3_grad_sumsq have filled, from
+ *              which norm and factor follow as in co3_grad_norm.  If the norm is not finite, state->skipped goes up instead,
+ *              and the step changes nothing
+ *   lr_dev     NULL, or a device float that stands for args->lr
  */
 int32_t co3_step_begin(const co3_adamw_args *args_host, const double *partials, int64_t count, const float *lr_dev,
                        co3_step_state *state, void *stream);
-int32_t co3_step_begin_norm(const co3_step_layout *layout_host, const void *plan, const co3_adamw_args *args_host, double *partials,
-                            const float *lr_dev, co3_step_state *state, void *stream);
 
 /*
  * AdamW on all tensors of a plan, with 32-bit (co3_adamw) or 8-bit states (co3_adamw8): one launch.
@@ -523,6 +522,17 @@ int32_t co3_adamw(const co3_step_layout *layout_host, const void *plan, float *m
                   const co3_adamw_args *args_host, const co3_step_state *state, void *stream);
 int32_t co3_adamw8(const co3_step_layout *layout_host, const void *plan, float *master, uint8_t *m, uint8_t *m_scale, uint8_t *r,
                    uint8_t *r_scale, const co3_adamw_args *args_host, const co3_step_state *state, void *stream);
+
+/*
+ * The step with its gradients clipped by their global norm, two launches: the results of co3_grad_sumsq, co3_step_begin and
+ * co3_adamw or co3_adamw8 for one table.  norm and factor are in the state afterwards; if the norm is not finite nothing
+ * changes but state->skipped.  partials: workspace as of co3_grad_sumsq; lr_dev as in co3_step_begin.
+ */
+int32_t co3_adamw_clipped(const co3_step_layout *layout_host, const void *plan, float *master, float *m, float *v,
+                          const co3_adamw_args *args_host, const float *lr_dev, double *partials, co3_step_state *state, void *stream);
+int32_t co3_adamw8_clipped(const co3_step_layout *layout_host, const void *plan, float *master, uint8_t *m, uint8_t *m_scale,
+                           uint8_t *r, uint8_t *r_scale, const co3_adamw_args *args_host, const float *lr_dev, double *partials,
+                           co3_step_state *state, void *stream);
 
 /* ---- launch timing (diagnostic) ------------------------------------------ */
 

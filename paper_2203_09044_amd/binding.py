@@ -32,7 +32,7 @@ EXPORTS = (
     "co3_user_encode_workspace_bytes", "co3_user_encode", "co3_set_exchange_spin_limit", "co3_design_layer_tables",
     "co3_ps_aggregate_partial", "co3_ps_decode_users", "co3_ps_average",
     "co3_step_layout_of", "co3_step_plan", "co3_grad_sumsq", "co3_grad_norm", "co3_step_begin",
-    "co3_step_begin_norm", "co3_adamw", "co3_adamw8",
+    "co3_adamw", "co3_adamw8", "co3_adamw_clipped", "co3_adamw8_clipped",
 )
 KERNEL_COUNT = 17
 TYPE_OF = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # CO3_F32, CO3_BF16, CO3_F16
@@ -164,12 +164,14 @@ def _load():
     L.co3_grad_norm.argtypes = [lay, p, C.c_double, C.c_double, p, p, p]
     L.co3_step_begin.restype = i32
     L.co3_step_begin.argtypes = [arg, p, i64, p, p, p]
-    L.co3_step_begin_norm.restype = i32
-    L.co3_step_begin_norm.argtypes = [lay, p, arg, p, p, p, p]
     L.co3_adamw.restype = i32
     L.co3_adamw.argtypes = [lay, p, p, p, p, arg, p, p]
     L.co3_adamw8.restype = i32
     L.co3_adamw8.argtypes = [lay, p, p, p, p, p, p, arg, p, p]
+    L.co3_adamw_clipped.restype = i32
+    L.co3_adamw_clipped.argtypes = [lay, p, p, p, p, arg, p, p, p, p]
+    L.co3_adamw8_clipped.restype = i32
+    L.co3_adamw8_clipped.argtypes = [lay, p, p, p, p, p, p, arg, p, p, p, p]
     L.co3_model_weights.restype = i32
     L.co3_model_weights.argtypes = [i32, _Fmt, C.c_double, C.c_double, p]
     L.co3_timing_enable.restype = i32
@@ -558,13 +560,6 @@ def step_begin(args: AdamwArgs, state, partials=None, count: Optional[int] = Non
                              _stream(stream)), "co3_step_begin")
 
 
-def step_begin_norm(layout: StepLayout, plan, args: AdamwArgs, state, partials, lr=None, stream=None):
-    """The same with the norm of the gradients of a plan, in one launch; partials: float64 workspace, zeroed once."""
-    _step_arrays(layout, plan, partials=(partials, layout.partials), state=(state, STEP_STATE_BYTES))
-    _chk(_lib.co3_step_begin_norm(C.byref(layout), _dp(plan, torch.uint8), C.byref(args), _dp(partials, torch.float64),
-                                  _dp(lr, torch.float32), _dp(state, torch.uint8), _stream(stream)), "co3_step_begin_norm")
-
-
 def adamw(layout: StepLayout, plan, m, v, args: AdamwArgs, state=None, master=None, stream=None):
     _step_arrays(layout, plan, m=(m, layout.elems), v=(v, layout.elems), master=(master, layout.elems), state=(state, STEP_STATE_BYTES))
     _chk(_lib.co3_adamw(C.byref(layout), _dp(plan, torch.uint8), _dp(master, torch.float32), _dp(m, torch.float32),
@@ -578,3 +573,23 @@ def adamw8(layout: StepLayout, plan, m, m_scale, r, r_scale, args: AdamwArgs, st
     e, s = torch.float8_e4m3fn, torch.float8_e8m0fnu
     _chk(_lib.co3_adamw8(C.byref(layout), _dp(plan, torch.uint8), _dp(master, torch.float32), _dp(m, e), _dp(m_scale, s), _dp(r, e),
                          _dp(r_scale, s), C.byref(args), _dp(state, torch.uint8), _stream(stream)), "co3_adamw8")
+
+
+def adamw_clipped(layout: StepLayout, plan, m, v, args: AdamwArgs, partials, state, master=None, lr=None, stream=None):
+    """partials: float64 workspace, zeroed once; lr: None, or one float32 on the device."""
+    _step_arrays(layout, plan, m=(m, layout.elems), v=(v, layout.elems), master=(master, layout.elems),
+                 partials=(partials, layout.partials), state=(state, STEP_STATE_BYTES))
+    _chk(_lib.co3_adamw_clipped(C.byref(layout), _dp(plan, torch.uint8), _dp(master, torch.float32), _dp(m, torch.float32),
+                                _dp(v, torch.float32), C.byref(args), _dp(lr, torch.float32), _dp(partials, torch.float64),
+                                _dp(state, torch.uint8), _stream(stream)), "co3_adamw_clipped")
+
+
+def adamw8_clipped(layout: StepLayout, plan, m, m_scale, r, r_scale, args: AdamwArgs, partials, state, master=None, lr=None, stream=None):
+    """The same with 8-bit states."""
+    _step_arrays(layout, plan, m=(m, layout.elems), r=(r, layout.elems), m_scale=(m_scale, layout.blocks),
+                 r_scale=(r_scale, layout.blocks), master=(master, layout.elems), partials=(partials, layout.partials),
+                 state=(state, STEP_STATE_BYTES))
+    e, s = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    _chk(_lib.co3_adamw8_clipped(C.byref(layout), _dp(plan, torch.uint8), _dp(master, torch.float32), _dp(m, e), _dp(m_scale, s),
+                                 _dp(r, e), _dp(r_scale, s), C.byref(args), _dp(lr, torch.float32), _dp(partials, torch.float64),
+                                 _dp(state, torch.uint8), _stream(stream)), "co3_adamw8_clipped")

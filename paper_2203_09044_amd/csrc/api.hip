@@ -768,7 +768,7 @@ int32_t co3_grad_norm(const co3_step_layout *layout, const void *plan, double gr
     return hip_rc(co3_launch_grad_sumsq(layout, plan, partials, f, static_cast<hipStream_t>(stream)));
 }
 
-static bool begin_ok(const co3_adamw_args *args, const float *lr_dev, const co3_step_state *state)
+static bool counted_ok(const co3_adamw_args *args, const float *lr_dev, const co3_step_state *state)
 {
     return adamw_args_ok(args) && state && aligned(state, 8) && (!lr_dev || aligned(lr_dev, 4));
 }
@@ -776,41 +776,47 @@ static bool begin_ok(const co3_adamw_args *args, const float *lr_dev, const co3_
 int32_t co3_step_begin(const co3_adamw_args *args, const double *partials, int64_t count, const float *lr_dev,
                        co3_step_state *state, void *stream)
 {
-    if (!begin_ok(args, lr_dev, state) || count < 0 || (partials && !aligned(partials, 8))) return CO3_EINVAL;
+    if (!counted_ok(args, lr_dev, state) || count < 0 || (partials && !aligned(partials, 8))) return CO3_EINVAL;
     const Co3StepFinish f{nullptr, reinterpret_cast<Co3StepDev *>(state), lr_dev, *args};
     return hip_rc(co3_launch_step_begin(partials, count, f, static_cast<hipStream_t>(stream)));
 }
 
-int32_t co3_step_begin_norm(const co3_step_layout *layout, const void *plan, const co3_adamw_args *args, double *partials,
-                            const float *lr_dev, co3_step_state *state, void *stream)
+// Checks of a step's arguments, and what all forms of it share.
+static bool step_of(const co3_step_layout *layout, const void *plan, int32_t state_bits, float *master, void *m, uint8_t *m_scale, void *v,
+                    uint8_t *v_scale, const co3_adamw_args *args, Co3StepLaunch &s)
 {
-    if (!layout_ok(layout, plan) || !partials || !aligned(partials, 8) || !begin_ok(args, lr_dev, state)) return CO3_EINVAL;
-    const Co3StepFinish f{nullptr, reinterpret_cast<Co3StepDev *>(state), lr_dev, *args};
-    return hip_rc(co3_launch_grad_sumsq(layout, plan, partials, f, static_cast<hipStream_t>(stream)));
+    if (!layout_ok(layout, plan) || layout->state_bits != state_bits || !adamw_args_ok(args)) return false;
+    if (!m || !v || !aligned(m, 4) || !aligned(v, 4) || (state_bits == 8 && (!m_scale || !v_scale))) return false;
+    if (master && (layout->param_type == CO3_F32 || !aligned(master, 4))) return false;
+    s = Co3StepLaunch{layout, plan, master, m, v, m_scale, v_scale, {}, {}, (float)args->grad_scale, nullptr};
+    s.fix = {(float)args->beta1, (float)(1.0 - args->beta1), (float)args->beta2, (float)(1.0 - args->beta2), (float)args->eps};
+    return true;
 }
 
 static int32_t adamw_common(const co3_step_layout *layout, const void *plan, int32_t state_bits, float *master, void *m,
                             uint8_t *m_scale, void *v, uint8_t *v_scale, const co3_adamw_args *args, const co3_step_state *state,
                             void *stream)
 {
-    if (!layout_ok(layout, plan) || layout->state_bits != state_bits || !adamw_args_ok(args)) return CO3_EINVAL;
-    if (!m || !v || !aligned(m, 4) || !aligned(v, 4) || (state_bits == 8 && (!m_scale || !v_scale))) return CO3_EINVAL;
-    if (master && (layout->param_type == CO3_F32 || !aligned(master, 4))) return CO3_EINVAL;
-    if (!state && args->t < 1) return CO3_EINVAL;
-    if (state && !aligned(state, 8)) return CO3_EINVAL;
-    Co3StepLaunch s{};
-    s.layout = layout;
-    s.plan = plan;
-    s.master = master;
-    s.m = m;
-    s.v = v;
-    s.m_scale = m_scale;
-    s.v_scale = v_scale;
-    s.fix = {(float)args->beta1, (float)(1.0 - args->beta1), (float)args->beta2, (float)(1.0 - args->beta2), (float)args->eps};
-    s.factor = (float)args->grad_scale;
+    Co3StepLaunch s;
+    if (!step_of(layout, plan, state_bits, master, m, m_scale, v, v_scale, args, s)) return CO3_EINVAL;
+    if (state ? !aligned(state, 8) : args->t < 1) return CO3_EINVAL;
     if (!state) s.var = co3_step_var(*args);
     s.state = state;
     return hip_rc(co3_launch_adamw(s, static_cast<hipStream_t>(stream)));
+}
+
+static int32_t clipped_common(const co3_step_layout *layout, const void *plan, int32_t state_bits, float *master, void *m,
+                              uint8_t *m_scale, void *v, uint8_t *v_scale, const co3_adamw_args *args, const float *lr_dev,
+                              double *partials, co3_step_state *state, void *stream)
+{
+    Co3StepLaunch s;
+    if (!step_of(layout, plan, state_bits, master, m, m_scale, v, v_scale, args, s)) return CO3_EINVAL;
+    if (!counted_ok(args, lr_dev, state) || !partials || !aligned(partials, 8)) return CO3_EINVAL;
+    s.state = state;
+    const Co3StepFinish f{nullptr, reinterpret_cast<Co3StepDev *>(state), lr_dev, *args};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (co3_launch_grad_sumsq(layout, plan, partials, f, st) != hipSuccess) return CO3_EHIP;
+    return hip_rc(co3_launch_adamw(s, st));
 }
 
 int32_t co3_adamw(const co3_step_layout *layout, const void *plan, float *master, float *m, float *v, const co3_adamw_args *args,
@@ -823,6 +829,19 @@ int32_t co3_adamw8(const co3_step_layout *layout, const void *plan, float *maste
                    uint8_t *r_scale, const co3_adamw_args *args, const co3_step_state *state, void *stream)
 {
     return adamw_common(layout, plan, 8, master, m, m_scale, r, r_scale, args, state, stream);
+}
+
+int32_t co3_adamw_clipped(const co3_step_layout *layout, const void *plan, float *master, float *m, float *v, const co3_adamw_args *args,
+                          const float *lr_dev, double *partials, co3_step_state *state, void *stream)
+{
+    return clipped_common(layout, plan, 32, master, m, nullptr, v, nullptr, args, lr_dev, partials, state, stream);
+}
+
+int32_t co3_adamw8_clipped(const co3_step_layout *layout, const void *plan, float *master, uint8_t *m, uint8_t *m_scale, uint8_t *r,
+                           uint8_t *r_scale, const co3_adamw_args *args, const float *lr_dev, double *partials, co3_step_state *state,
+                           void *stream)
+{
+    return clipped_common(layout, plan, 8, master, m, m_scale, r, r_scale, args, lr_dev, partials, state, stream);
 }
 
 // ---- model table (host arithmetic only) ---------------------------------------------------

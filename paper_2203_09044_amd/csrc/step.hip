@@ -281,21 +281,19 @@ __global__ __launch_bounds__(ST_BLOCK) void k_adamw(const Co3StepChunk *__restri
 {
     constexpr int V = 4;
     const Co3StepChunk ch = plan[blockIdx.x];
-    const Co3StepNow now = step_now(ch, var, factor, dev);
-    if (now.factor < 0.0f) return;
     const auto p = at<P>(ch.param);
     const auto g = at<G>(ch.grad);
     const auto w32 = at<CO3_F32>(MASTER ? master_all + ch.state : nullptr);
     const auto m = at<CO3_F32>(m_all + ch.state), v = at<CO3_F32>(v_all + ch.state);
     float gx[ST_GROUPS][V], mx[ST_GROUPS][V], vx[ST_GROUPS][V], wx[ST_GROUPS][V];
-    auto step = [&](int k) {
+    const int i = threadIdx.x * V;
+    auto step = [&](const Co3StepNow &now, int k) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             step_moments(c, now.factor, gx[k][e], mx[k][e], vx[k][e]);
             wx[k][e] = step_weight(c, now.rbc2, now.decay, now.step, wx[k][e], mx[k][e], __builtin_sqrtf(vx[k][e]));
         }
     };
-    const int i = threadIdx.x * V;
     if (ch.count == ST_GROUPS * ST_BLOCK * V) {
 #pragma unroll
         for (int k = 0; k < ST_GROUPS; ++k) {
@@ -306,16 +304,20 @@ __global__ __launch_bounds__(ST_BLOCK) void k_adamw(const Co3StepChunk *__restri
             if (MASTER) Elems<CO3_F32>::load<V>(w32 + j, wx[k]);
             else Elems<P>::template load<V>(p + j, wx[k]);
         }
+        const Co3StepNow now = step_now(ch, var, factor, dev);
+        if (now.factor < 0.0f) return;
 #pragma unroll
         for (int k = 0; k < ST_GROUPS; ++k) {
             const int j = i + k * ST_BLOCK * V;
-            step(k);
+            step(now, k);
             Elems<CO3_F32>::store<V>(m + j, mx[k]);
             Elems<CO3_F32>::store<V>(v + j, vx[k]);
             if (MASTER) Elems<CO3_F32>::store<V>(w32 + j, wx[k]);
             Elems<P>::template store<V>(p + j, wx[k]);
         }
     } else {
+        const Co3StepNow now = step_now(ch, var, factor, dev);
+        if (now.factor < 0.0f) return;
         for (int j = i; j < ch.count; j += ST_BLOCK * V) {
             const int here = ch.count - j;
             load_some<G, V>(g + j, here, gx[0]);
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(ST_BLOCK) void k_adamw(const Co3StepChunk *__restri
             load_some<CO3_F32, V>(v + j, here, vx[0]);
             if (MASTER) load_some<CO3_F32, V>(w32 + j, here, wx[0]);
             else load_some<P, V>(p + j, here, wx[0]);
-            step(0);
+            step(now, 0);
             store_some<CO3_F32, V>(m + j, here, mx[0]);
             store_some<CO3_F32, V>(v + j, here, vx[0]);
             if (MASTER) store_some<CO3_F32, V>(w32 + j, here, wx[0]);

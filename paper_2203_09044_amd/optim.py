@@ -232,7 +232,8 @@ class AdamW:
         # an array of no elements has no address: any will do, none is read
         self._state_ptrs = [C.c_void_p(s.data_ptr() or t.plan.data_ptr()) for s in states]
         self._master_ptr = None if self.master is None else C.c_void_p(self.master.data_ptr() or t.plan.data_ptr())
-        self._step_fn = B._lib.co3_adamw if state_bits == 32 else B._lib.co3_adamw8
+        self._step_fn, self._clipped_fn = ((B._lib.co3_adamw, B._lib.co3_adamw_clipped) if state_bits == 32 else
+                                           (B._lib.co3_adamw8, B._lib.co3_adamw8_clipped))
         self._t = 0
         self._dev = torch.zeros(B.STEP_STATE_BYTES // 8, dtype=torch.int64, **z)
         self._dev_ptr = C.c_void_p(self._dev.data_ptr())
@@ -332,18 +333,17 @@ class AdamW:
         """One step on every tensor.  ``grads``: None, or tensors of the same sizes to take instead, from now on."""
         t = self._table
         stream = t.ready(grads, self._device_steps)
-        state = None
-        if self._device_steps:
-            state = self._dev_ptr
-            if self.max_norm is not None:
-                B._chk(B._lib.co3_step_begin_norm(t.layout_ref, t.plan_ptr, self._args_ref, self._partials_ptr, self._lr_ptr, state, stream),
-                       "co3_step_begin_norm")
-            else:
-                B._chk(B._lib.co3_step_begin(self._args_ref, None, 0, self._lr_ptr, state, stream), "co3_step_begin")
+        if self.max_norm is not None:
+            B._chk(self._clipped_fn(t.layout_ref, t.plan_ptr, self._master_ptr, *self._state_ptrs, self._args_ref, self._lr_ptr,
+                                    self._partials_ptr, self._dev_ptr, stream), "co3_adamw_clipped")
         else:
-            self._args.t = self._t + 1
-        B._chk(self._step_fn(t.layout_ref, t.plan_ptr, self._master_ptr, *self._state_ptrs, self._args_ref, state, stream),
-               "co3_adamw" if self.state_bits == 32 else "co3_adamw8")
-        if state is None:
-            self._t += 1
+            state = None
+            if self._device_steps:
+                state = self._dev_ptr
+                B._chk(B._lib.co3_step_begin(self._args_ref, None, 0, self._lr_ptr, state, stream), "co3_step_begin")
+            else:
+                self._args.t = self._t + 1
+            B._chk(self._step_fn(t.layout_ref, t.plan_ptr, self._master_ptr, *self._state_ptrs, self._args_ref, state, stream), "co3_adamw")
+            if state is None:
+                self._t += 1
         torch.autograd.graph.increment_version(t.params)       # written in place, though not by torch

@@ -550,6 +550,33 @@ def test_the_separate_calls_make_the_step(co3):
                    1e-3, (0.9, 0.999), 1e-8, [0.01] * len(sizes), [1.0] * len(sizes), 11)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_clipped_call_is_the_separate_ones(co3, bits):
+    B = co3.binding
+    results = []
+    for together in (True, False):
+        torch.manual_seed(9)
+        params = [torch.randn(n, device="cuda") for n in (300_000, 7)]
+        opt = co3.AdamW(params, [torch.randn_like(p) for p in params], state_bits=bits)
+        t = opt._table
+        partials = torch.zeros(t.layout.partials, dtype=torch.float64, device="cuda")
+        state = torch.zeros(64, dtype=torch.uint8, device="cuda")
+        args = B.AdamwArgs(0.0, 0.9, 0.999, 1e-8, 2.0, 0.5, 0, 12)
+        lr = torch.tensor([1e-2], device="cuda")
+        s = (opt.m, opt.v) if bits == 32 else (opt.m, opt.m_scale, opt.r, opt.r_scale)
+        for _ in range(3):
+            if together:
+                (B.adamw_clipped if bits == 32 else B.adamw8_clipped)(t.layout, t.plan, *s, args, partials, state, lr=lr)
+            else:
+                B.grad_sumsq(t.layout, t.plan, partials)
+                B.step_begin(args, state, partials, lr=lr)
+                (B.adamw if bits == 32 else B.adamw8)(t.layout, t.plan, *s, args, state=state)
+        assert int(state.view(torch.int64)[0]) == 3
+        results.append(params + [x.view(torch.uint8) for x in s] + [state.view(torch.float32)[4:6]])
+    # the sums are added in another order: the factor may be another rounding of the same number, here it is not
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
 @pytest.mark.parametrize("bits,ptype,n", [(32, F32, (1 << 30) + 1027), (8, BF16, (1 << 31) + 1300)])
 def test_offsets_beyond_32_bits(co3, bits, ptype, n):
     """One tensor whose arrays are longer than 2^32 bytes (the parameters; with 8-bit states the states' places pass 2^31): its

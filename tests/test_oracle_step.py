@@ -126,6 +126,7 @@ def test_plan_covers_every_element_once(B, bits, pt, gt, sizes):
     assert L.chunk % 256 == 0 and L.partials >= 2
     plan = B.step_plan(t, L).numpy()
     assert plan.nbytes == L.plan_bytes
+    assert L.plan_bytes == (40 * L.chunks or 16)
     entries = plan[:L.chunks * 40].view(np.dtype([("p", "<u8"), ("g", "<u8"), ("at", "<i8"), ("n", "<i4"), ("ls", "<f4"), ("wd", "<f4"), ("x", "<i4")]))
     k = 0
     for n, x, at in zip(sizes, t, starts):
@@ -197,7 +198,8 @@ def test_device_calls_refuse_bad_arguments_on_the_host(B):
         assert lib.co3_adamw8(C.byref(L8), p, None, p, p, p, p, args(**kw), None, None) == B.EINVAL, kw
         if "t" not in kw:
             assert lib.co3_step_begin(args(**kw), None, 0, None, p, None) == B.EINVAL, kw
-            assert lib.co3_step_begin_norm(C.byref(L32), p, args(**kw), p, None, p, None) == B.EINVAL, kw
+            assert lib.co3_adamw_clipped(C.byref(L32), p, None, p, p, args(**kw), None, p, p, None) == B.EINVAL, kw
+            assert lib.co3_adamw8_clipped(C.byref(L8), p, None, p, p, p, p, args(**kw), None, p, p, None) == B.EINVAL, kw
     for a in ((None, p, None, p, p), (C.byref(L32), None, None, p, p), (C.byref(L8), p, None, p, p), (C.byref(L0), p, None, p, p),
               (C.byref(L32), p, p, p, p), (C.byref(L32), p, None, None, p), (C.byref(L32), p, None, p, None),
               (C.byref(L32), p, None, odd, p), (C.byref(L32), odd, None, p, p)):
@@ -211,10 +213,14 @@ def test_device_calls_refuse_bad_arguments_on_the_host(B):
               (C.byref(L0), p, 1.0, 0.0, p, p), (C.byref(L0), p, math.nan, 1.0, p, p), (C.byref(L0), p, 1.0, math.nan, p, p),
               (None, p, 1.0, 1.0, p, p), (C.byref(L0), None, 1.0, 1.0, p, p), (C.byref(L0), p, 1.0, 1.0, p, odd)):
         assert lib.co3_grad_norm(*a, None) == B.EINVAL
-    for a in ((None, p, args(), p, None, p), (C.byref(L32), None, args(), p, None, p), (C.byref(L32), p, None, p, None, p),
-              (C.byref(L32), p, args(), None, None, p), (C.byref(L32), p, args(), odd, None, p), (C.byref(L32), p, args(), p, odd, p),
-              (C.byref(L32), p, args(), p, None, None), (C.byref(L32), p, args(), p, None, odd)):
-        assert lib.co3_step_begin_norm(*a, None) == B.EINVAL
+    for a in ((None, p, p), (odd, p, p), (p, None, p), (p, odd, p)):          # partials, state, moments
+        assert lib.co3_adamw_clipped(C.byref(L32), p, None, a[2], a[2], args(), None, a[0], a[1], None) == B.EINVAL
+        assert lib.co3_adamw8_clipped(C.byref(L8), p, None, p, p, p, p, args(), None, a[0], a[1], None) == B.EINVAL
+    assert lib.co3_adamw_clipped(C.byref(L32), p, None, p, p, args(), odd, p, p, None) == B.EINVAL
+    assert lib.co3_adamw_clipped(C.byref(L8), p, None, p, p, args(), None, p, p, None) == B.EINVAL
+    assert lib.co3_adamw_clipped(C.byref(L32), p, p, p, p, args(), None, p, p, None) == B.EINVAL
+    assert lib.co3_adamw_clipped(None, p, None, p, p, args(), None, p, p, None) == B.EINVAL
+    assert lib.co3_adamw8_clipped(C.byref(L8), p, None, p, None, p, p, args(), None, p, p, None) == B.EINVAL
     assert lib.co3_grad_sumsq(C.byref(L0), p, None, None) == B.EINVAL
     for a in ((args(), None, 0, None, None), (args(), None, -1, None, p), (args(), odd, 1, None, p), (args(), None, 0, odd, p),
               (args(), None, 0, None, odd), (None, None, 0, None, p)):
