@@ -407,10 +407,10 @@ void co3_set_exchange_spin_limit(int64_t polls);
  * Step t, every operation on its own rounded to fp32, scalars computed in fp64 and rounded once:
  *     g' = factor * g;   m' = beta1 m + (1 - beta1) g';   v' = beta2 v + (1 - beta2) (g' g')
  *     p' = p - ((lr_s weight_decay) p + (lr_s / (1 - beta1^t)) (m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)))
- * with lr_s = lr * lr_scale of the tensor (sqrt correctly rounded, the quotient by 1 / sqrt(1 - beta2^t) a product, that by the
- * divisor within two units in the last place).  Parameters and gradients are
- * fp32, bf16 or fp16; a 16-bit parameter is rounded to nearest, ties to even, from the fp32 result, and the step starts
- * from it, or, where a master array is given, from the fp32 value kept there (the parameter is then written only).
+ * with lr_s = lr * lr_scale of the tensor (sqrt is correctly rounded; the quotient by sqrt(1 - beta2^t) is a product, the other
+ * one within two units in the last place).  Parameters and gradients are fp32, bf16 or fp16; a 16-bit parameter is rounded
+ * to nearest, ties to even, from the fp32 result, and the step starts from it, or, where a master array is given, from
+ * the fp32 value kept there (the parameter is then written only).
  *
  * Places.  The tensors of a call lie one behind another in the state arrays (moments, masters), in the order of the
  * table: packed for 32-bit states, each begun at a multiple of 256 places for 8-bit ones.  co3_step_layout_of says how
@@ -462,8 +462,8 @@ typedef struct {
 } co3_adamw_args;
 
 /* Device memory of the caller, 8-byte aligned, zeroed once: what a step that the device counts goes by.  t is the number of steps
- * taken, skipped how many were left out; norm and factor are those of the last step that took a norm.  The rest is the
- * library's. */
+ * taken, skipped how many were left out; norm (0 where none was taken) and factor are those of the step begun last.  The rest
+ * is the library's. */
 typedef struct {
     int64_t t, skipped;
     float norm, factor;

@@ -22,6 +22,14 @@ PerTensor = Union[float, Sequence[float]]
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
+def _same_addresses(tensors, addresses, places):
+    return [t.data_ptr() for t in tensors] == addresses
+
+
+# the same in one call where torch has it (28 ns a tensor against 42)
+_same_addresses = getattr(torch._C, "_tensors_data_ptrs_at_indices_equal", _same_addresses)
+
+
 def _per_tensor(x: PerTensor, T: int, what: str) -> List[float]:
     values = [float(x)] * T if isinstance(x, (int, float)) else [float(v) for v in x]
     if len(values) != T:
@@ -39,16 +47,15 @@ def _check_scale(grad_scale: float):
 def _check_tensors(tensors: Sequence[torch.Tensor], what: str):
     if not tensors:
         raise ValueError(f"no {what}")
-    first = tensors[0]
-    for t in tensors:
-        if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
-            raise ValueError(f"{what}: CUDA tensors are needed")
-        if t.dtype not in B.TYPE_OF or t.dtype != first.dtype:
-            raise ValueError(f"{what}: all of one type out of float32, bfloat16 and float16 (a handle per type where a model mixes them)")
-        if t.device != first.device:
-            raise ValueError(f"{what}: all on one device")
-        if not t.is_contiguous():
-            raise ValueError(f"{what}: contiguous tensors are needed")
+    if not all(isinstance(t, torch.Tensor) and t.is_cuda for t in tensors):
+        raise ValueError(f"{what}: CUDA tensors are needed")
+    dtype, device = tensors[0].dtype, tensors[0].get_device()
+    if dtype not in B.TYPE_OF or not all(t.dtype is dtype for t in tensors):
+        raise ValueError(f"{what}: all of one type out of float32, bfloat16 and float16 (a handle per type where a model mixes them)")
+    if not all(t.get_device() == device for t in tensors):
+        raise ValueError(f"{what}: all on one device")
+    if not all(t.is_contiguous() for t in tensors):
+        raise ValueError(f"{what}: contiguous tensors are needed")
 
 
 class _Table:
@@ -72,10 +79,6 @@ class _Table:
         self._check(grads)
         self.sizes = [g.numel() for g in grads]
         self.grads = grads
-        self._watch()
-
-    def _watch(self):
-        self._where = [t.data_ptr for t in self.grads + (self.params or [])]
 
     def _check(self, grads: Sequence[torch.Tensor]):
         _check_tensors(grads, "gradients")
@@ -89,12 +92,10 @@ class _Table:
         if sizes != [g.numel() for g in grads]:
             raise ValueError("gradients: one per parameter, with as many elements")
 
-    def _addresses(self) -> List[int]:
-        return [f() for f in self._where]
-
     def _make(self):
-        self._check(self.grads)
-        at, T = self._addresses(), len(self.grads)
+        T = len(self.grads)
+        watched = self.grads + (self.params or [])
+        at = [t.data_ptr() for t in watched]
         rows = (B.StepTensor * T)()
         for k, n in enumerate(self.sizes):
             rows[k] = B.StepTensor(None if self.params is None else at[T + k], at[k], n, self.lr_scales[k], self.weight_decays[k])
@@ -108,7 +109,8 @@ class _Table:
             self.plan = host.to(self.device)
             self._streams = {_raw_stream(self.device.index)}     # streams that the memory is known to
         self.layout, self.layout_ref, self.plan_ptr = layout, C.byref(layout), C.c_void_p(self.plan.data_ptr())
-        self._at, self._dtype = at, self.grads[0].dtype          # what the plan is for
+        self._watched, self._at, self._places = watched, at, list(range(len(at)))     # what the plan is for
+        self._dtype = self.grads[0].dtype
 
     def ready(self, grads: Optional[Sequence[torch.Tensor]], capturable: bool = True) -> C.c_void_p:
         """The plan is that of the tensors as they lie now; returns the current stream of their device, which is the current one."""
@@ -118,14 +120,17 @@ class _Table:
         was = self.grads
         if grads is not None:
             self._take(grads)
-        if self._at != self._addresses() or self._dtype != self.grads[0].dtype:
+            self._watched = self.grads + (self.params or [])
+        if not _same_addresses(self._watched, self._at, self._places) or self.grads[0].dtype != self._dtype:
             try:
                 if capturing:
                     raise RuntimeError("a tensor has moved since the last call: call once before the capture")
+                if grads is None:
+                    self._check(self.grads)
                 self._make()
             except Exception:
                 self.grads = was                                 # refused gradients are not kept
-                self._watch()
+                self._watched = was + (self.params or [])
                 raise
         raw = _raw_stream(self.device.index)
         if capturing:
@@ -294,8 +299,7 @@ class AdamW:
     def take_masters(self):
         """Masters as the parameters are now (after the parameters were loaded from elsewhere)."""
         if self.master is not None:
-            for w, p in zip(self._views(self.master), self._table.params):
-                w.copy_(p.detach())
+            torch._foreach_copy_(self._views(self.master), [p.detach() for p in self._table.params])
 
     def moments(self):
         """(m, v) of every tensor as float32 copies, whatever the states are kept in."""
