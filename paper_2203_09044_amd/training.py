@@ -13,6 +13,9 @@ corrected gradients (no symbol statistics), refreshed every ``refresh`` iteratio
 refreshes the user side runs in one pass (conversion and compression without a symbol array).
 ``tables="lagged"``: per-user Huffman codes from the previous iteration's symbol counts, which the
 one-pass user side gathers on the way.
+
+``max_norm`` scales the averaged reconstruction down to a global norm before the step; ``Co3AdamW`` takes the step
+with AdamW instead, all tensors in one pass.
 """
 from __future__ import annotations
 
@@ -24,14 +27,14 @@ from co3_inputs import group_small_tensors, seg_offsets
 
 from . import binding as B
 from .binding import Fmt
-from .optim import AdamW
+from .optim import AdamW, GradNorm
 from .pipeline import Co3Pipeline
 
 
 class Co3SGD:
     def __init__(self, model: torch.nn.Module, users: int, fmt: Fmt, lr: float, gamma: float = 1.0,
                  chunk_syms: int = 256, bias: str = "absmax", codes: str = "user", code_group_min: int = 16384,
-                 tables: str = "empirical", refresh: int = 10, cap_words: Optional[int] = None):
+                 tables: str = "empirical", refresh: int = 10, cap_words: Optional[int] = None, max_norm: Optional[float] = None):
         if tables not in ("empirical", "model", "lagged"):
             raise ValueError("tables must be 'empirical', 'model' or 'lagged'")
         if tables == "model" and (bias != "moments" or codes != "layer"):
@@ -71,6 +74,8 @@ class Co3SGD:
         self.err_before = torch.empty_like(self.pipe.err) if self.pipe.single_pass else None
         self.codes_before = torch.empty_like(self.pipe.codes) if self.pipe.single_pass else None
         self.capacity_growths = 0
+        # the averaged reconstruction is scaled down to this global norm before the step (None: taken as it is)
+        self.norm = None if max_norm is None else GradNorm([self.pipe.avg[:self.n]], max_norm=max_norm)
 
     def local_gradients(self, batches: Sequence[Tuple[torch.Tensor, torch.Tensor]],
                         loss_fn: Callable[[torch.Tensor, torch.Tensor], torch.Tensor]) -> float:
@@ -95,6 +100,9 @@ class Co3SGD:
     def apply_average(self, avg: Optional[torch.Tensor] = None):
         """Parameter-server update with the averaged reconstruction (Algorithm 1, last step)."""
         avg = self.pipe.avg if avg is None else avg
+        if self.norm is not None:                  # (norm, factor); the factor of a norm that is not finite is -1: no step
+            factor = self.norm.compute([avg[:self.n]])[1]
+            avg = torch.where(factor > 0.0, avg[:self.n] * factor, 0.0)
         with torch.no_grad():
             for p, a, b in zip(self.params, self.seg_off[:-1], self.seg_off[1:]):
                 p.add_(avg[a:b].view_as(p), alpha=-self.lr)

@@ -648,6 +648,34 @@ def test_training_steps_the_model_with_the_averaged_reconstruction(co3, bits, ma
     assert opt.opt.t == 3
 
 
+def test_sgd_takes_the_clipped_average(co3):
+    """Co3SGD with max_norm: the step is that of the average scaled to the norm; without it, or below it, the average's own."""
+    loss = torch.nn.functional.cross_entropy
+    for max_norm in (1e-2, 1e6, None):
+        model, sample = problem()
+        opt = co3.Co3SGD(model, 2, co3.Fmt(4, 3), lr=0.1, max_norm=max_norm)
+        for t in range(2):
+            before = [p.detach().clone() for p in opt.params]
+            opt.step([sample(t, u) for u in range(2)], loss)
+            avg = opt.pipe.avg[:opt.n]
+            norm, c = O.norm([avg.double().cpu().numpy()], 1.0, max_norm or math.inf)
+            if max_norm is not None:
+                got = opt.norm.compute().cpu().numpy()
+                assert abs(got[0] - norm) <= U * (1 + 1e-6) * norm
+                c = float(got[1])
+            for p, b, a0, a1 in zip(opt.params, before, opt.seg_off[:-1], opt.seg_off[1:]):
+                want = torch.add(b, (avg[a0:a1] * torch.tensor(c, device="cuda") if max_norm else avg[a0:a1]).view_as(p), alpha=-0.1)
+                assert torch.equal(p.detach(), want)
+        assert (max_norm == 1e-2) == (c < 1.0)
+    # a norm that is not finite: no step
+    bad = torch.full((opt.n,), 1.0, device="cuda")
+    bad[3] = math.nan
+    clipped = co3.Co3SGD(model, 2, co3.Fmt(4, 3), lr=0.1, max_norm=1.0)
+    before = [p.detach().clone() for p in clipped.params]
+    clipped.apply_average(bad)
+    assert all(torch.equal(p.detach(), b) for p, b in zip(clipped.params, before))
+
+
 def test_training_with_another_average_and_rate(co3):
     model, sample = problem()
     opt = co3.Co3AdamW(model, 2, co3.Fmt(3, 1), lr=1e-2)
