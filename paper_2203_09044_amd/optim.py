@@ -198,7 +198,8 @@ class AdamW:
     grad_scale      multiplies every gradient (1 / loss scale, say)
     device_steps    the device counts the steps, which a captured step needs (always so with max_norm or a tensor ``lr``)
 
-    The state arrays hold the tensors one behind another: packed with 32 bits, each from a multiple of 256 on with 8.
+    The state arrays hold the tensors one behind another: packed with 32 bits, each from a multiple of 256 on with 8.  They stay the
+    handle's: a program copies into them.  A graph that holds a captured step needs the handle alive.
     """
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: Union[float, torch.Tensor] = 1e-3,

@@ -103,7 +103,7 @@ def check_step(opt, sizes, before, after_params, grads, masters_before, t, facto
 
 
 TABLES = {"one": [1], "tiny": [3, 0, 5, 1, 2], "blocks": [255, 256, 257, 1, 0, 511, 512, 513], "chunks": [1023, 1024, 1025, 4095, 4097],
-          "mixed": [10_000, 64, 64, 1, 70_003, 0, 10]}
+          "mixed": [10_000, 64, 64, 1, 70_003, 0, 10], "many": [64, 1, 300, 5] * 150}
 TYPES = [(F32, F32, False), (F32, BF16, False), (BF16, BF16, False), (BF16, F32, True), (F16, F16, True), (F16, F32, False)]
 
 
@@ -294,6 +294,52 @@ def test_norm_at_the_ends_of_the_range(co3):
     for bad in (math.inf, math.nan):
         small[3] = bad
         assert float(co3.GradNorm([small]).compute()[1]) == -1.0
+
+
+def test_replays_of_captured_norms(co3):
+    """Two graphs of one handle, eager calls between their replays: every norm is that of the gradients as they are then."""
+    g = [torch.randn(n, device="cuda") for n in (100_000, 3, 5_000)]
+    handle = co3.GradNorm(g, max_norm=1.0)
+    graphs, outs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for graph in graphs:
+        with torch.cuda.graph(graph):
+            outs.append(handle.compute().clone())
+    for t in range(4):
+        for graph, out in zip(graphs, outs):
+            for x in g:
+                x.mul_(1.25 + t)
+            want = co3.GradNorm(g, max_norm=1.0).compute().clone()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.rand(1 << 20, device="cuda").sum().item() > 0
+            assert torch.equal(out, want) and torch.equal(handle.compute(), want)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_separate_calls_leave_out_a_step_whose_norm_is_not_finite(co3, bad):
+    B = co3.binding
+    params = [torch.randn(5000, device="cuda"), torch.randn(300, device="cuda").to(BF16)]
+    grads = [torch.randn_like(p) for p in params]
+    opts = [co3.AdamW([p], [g], state_bits=b) for p, g, b in zip(params, grads, (8, 32))]
+    layouts, plans = [o._table.layout for o in opts], [o._table.plan for o in opts]
+    partials = torch.zeros(sum(L.partials for L in layouts), dtype=torch.float64, device="cuda")
+    state = torch.zeros(64, dtype=torch.uint8, device="cuda")
+    args = B.AdamwArgs(1e-3, 0.9, 0.999, 1e-8, 1.0, 1.0, 0, 1)
+    for t, poison in enumerate((None, bad, None)):
+        keep = [x.view(torch.uint8).clone() for x in params] + [x.view(torch.uint8).clone() for o in opts for x in o._named().values()]
+        old = grads[1][17].clone()
+        if poison is not None:
+            grads[1][17] = poison
+        B.grad_sumsq(layouts[0], plans[0], partials[:layouts[0].partials])
+        B.grad_sumsq(layouts[1], plans[1], partials[layouts[0].partials:])
+        B.step_begin(args, state, partials)
+        B.adamw8(layouts[0], plans[0], opts[0].m, opts[0].m_scale, opts[0].r, opts[0].r_scale, args, state=state)
+        B.adamw(layouts[1], plans[1], opts[1].m, opts[1].v, args, state=state)
+        now = [x.view(torch.uint8) for x in params] + [x.view(torch.uint8) for o in opts for x in o._named().values()]
+        same = [torch.equal(a, b) for a, b in zip(keep, now)]
+        assert all(same) if poison is not None else not any(same[:2])
+        grads[1][17] = old
+    assert state.view(torch.int64)[:2].tolist() == [2, 1]
 
 
 @pytest.mark.parametrize("bits", [32, 8])
@@ -646,6 +692,20 @@ def test_training_steps_the_model_with_the_averaged_reconstruction(co3, bits, ma
         check_step(opt.opt, sizes, before, [p.detach().reshape(-1).float().cpu().numpy() for p in opt.params], grads, w, t, factor, 1e-2,
                    (0.9, 0.999), 1e-8, decays, [1.0] * len(sizes), 21)
     assert opt.opt.t == 3
+
+
+@pytest.mark.parametrize("tables,codes,bias", [("lagged", "user", "absmax"), ("model", "layer", "moments")])
+def test_adamw_behind_every_form_of_the_codec(co3, tables, codes, bias):
+    model, sample = problem()
+    opt = co3.Co3AdamW(model, 2, co3.Fmt(3, 1), lr=1e-2, state_bits=8, max_norm=1.0, tables=tables, codes=codes, bias=bias,
+                       code_group_min=10000, refresh=2)
+    for t in range(4):
+        before = [p.detach().clone() for p in opt.params]
+        assert math.isfinite(opt.step([sample(t, u) for u in range(2)], torch.nn.functional.cross_entropy))
+        norm = float(torch.linalg.vector_norm(opt.pipe.avg[:opt.n].double()))
+        assert abs(float(opt.opt.norm[0]) - norm) <= U * (1 + 1e-6) * norm
+        assert not any(torch.equal(p.detach(), b) for p, b in zip(opt.params, before))
+    assert opt.opt.t == 4 and opt.pipe.poll() == 0
 
 
 def test_sgd_takes_the_clipped_average(co3):
