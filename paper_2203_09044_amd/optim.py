@@ -12,6 +12,7 @@ import functools
 import math
 from typing import List, Optional, Sequence, Union
 
+import numpy as np
 import torch
 
 from . import binding as B
@@ -96,9 +97,12 @@ class _Table:
         T = len(self.grads)
         watched = self.grads + (self.params or [])
         at = [t.data_ptr() for t in watched]
-        rows = (B.StepTensor * T)()
-        for k, n in enumerate(self.sizes):
-            rows[k] = B.StepTensor(None if self.params is None else at[T + k], at[k], n, self.lr_scales[k], self.weight_decays[k])
+        table = np.zeros(T, dtype=[("param", "u8"), ("grad", "u8"), ("n", "i8"), ("lr_scale", "f4"), ("weight_decay", "f4")])
+        if self.params is not None:
+            table["param"] = at[T:]
+        table["grad"], table["n"] = at[:T], self.sizes
+        table["lr_scale"], table["weight_decay"] = self.lr_scales, self.weight_decays
+        rows = (B.StepTensor * T).from_buffer(table)
         layout = B.step_layout_of(rows, B.TYPE_NONE if self.params is None else B.TYPE_OF[self.params[0].dtype],
                                   B.TYPE_OF[self.grads[0].dtype], self.state_bits)
         try:
@@ -291,11 +295,11 @@ class AdamW:
         return int(self._dev[1].item())
 
     def _views(self, flat: torch.Tensor) -> List[torch.Tensor]:
-        unit, at, out = B.STEP_BLOCK if self.state_bits == 8 else 1, 0, []
-        for p in self._table.params:
-            out.append(flat[at:at + p.numel()].view(p.shape))
-            at += (p.numel() + unit - 1) // unit * unit
-        return out
+        unit, sizes = B.STEP_BLOCK if self.state_bits == 8 else 1, self._table.sizes
+        parts = flat.split([(n + unit - 1) // unit * unit for n in sizes])
+        if unit > 1:
+            parts = [x[:n] for x, n in zip(parts, sizes)]
+        return [x if p.dim() == 1 else x.view(p.shape) for x, p in zip(parts, self._table.params)]
 
     def take_masters(self):
         """Masters as the parameters are now (after the parameters were loaded from elsewhere)."""
