@@ -10,5 +10,5 @@ Importing the package requires the built library: there is no CPU fallback.
 from . import binding  # noqa: F401  (raises ImportError when libco3.so is missing)
 from .binding import Fmt, Co3Error  # noqa: F401
 from .pipeline import Co3Pipeline  # noqa: F401
-from .optim import AdamW, GradNorm  # noqa: F401
+from .optim import AdamW, GradNorm, MixedAdamW  # noqa: F401
 from .training import Co3AdamW, Co3SGD  # noqa: F401

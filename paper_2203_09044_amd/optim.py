@@ -52,11 +52,24 @@ def _check_tensors(tensors: Sequence[torch.Tensor], what: str):
         raise ValueError(f"{what}: CUDA tensors are needed")
     dtype, device = tensors[0].dtype, tensors[0].get_device()
     if dtype not in B.TYPE_OF or not all(t.dtype is dtype for t in tensors):
-        raise ValueError(f"{what}: all of one type out of float32, bfloat16 and float16 (a handle per type where a model mixes them)")
+        raise ValueError(f"{what}: all of one type out of float32, bfloat16 and float16 (MixedAdamW takes several)")
     if not all(t.get_device() == device for t in tensors):
         raise ValueError(f"{what}: all on one device")
     if not all(t.is_contiguous() for t in tensors):
         raise ValueError(f"{what}: contiguous tensors are needed")
+
+
+def _overlapping(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor]) -> bool:
+    """Whether a parameter shares memory with another one or with a gradient."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), kind) for kind, ts in enumerate((params, grads)) for t in ts
+                   if t.numel())
+    end_any = end_param = 0
+    for lo, hi, kind in spans:
+        if lo < end_param or (kind == 0 and lo < end_any):
+            return True
+        end_any = max(end_any, hi)
+        end_param = max(end_param, hi) if kind == 0 else end_param
+    return False
 
 
 class _Table:
@@ -356,3 +369,110 @@ class AdamW:
             if state is None:
                 self._t += 1
         torch.autograd.graph.increment_version(t.params)       # written in place, though not by torch
+
+
+class MixedAdamW:
+    """AdamW over parameters of several types, as of a 16-bit model with 32-bit norms: one part (``AdamW``) per pair of parameter and
+    gradient type, all of them one step, clipped by one norm.  Arguments as of ``AdamW``; ``master`` is for the 16-bit parts.
+    ``parts`` hold the states, ``places[k]`` says which of the parameters part k has; the device counts the steps."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: Union[float, torch.Tensor] = 1e-3,
+                 weight_decay: PerTensor = 0.01, lr_scales: PerTensor = 1.0, master: bool = False, max_norm: Optional[float] = None, **kw):
+        params, grads = list(params), list(grads)
+        if not params or len(params) != len(grads) or not all(isinstance(t, torch.Tensor) for t in params + grads):
+            raise ValueError("gradients: one per parameter")
+        if any(p.device != params[0].device for p in params):
+            raise ValueError("parameters: all on one device")
+        if max_norm is not None and not max_norm > 0.0:
+            raise ValueError("max_norm must be positive")
+        decays, scales = _per_tensor(weight_decay, len(params), "weight_decay"), _per_tensor(lr_scales, len(params), "lr_scales")
+        kw.pop("device_steps", None)                                # always so
+        if _overlapping(params, grads):
+            raise ValueError("a parameter shares memory with another one or with a gradient")
+        kinds = {}
+        for k, (p, g) in enumerate(zip(params, grads)):
+            kinds.setdefault((p.dtype, g.dtype), []).append(k)
+        self.places = list(kinds.values())
+        pick = lambda values, places: [values[k] for k in places]  # noqa: E731
+        self.parts = [AdamW(pick(params, places), pick(grads, places), lr=lr, weight_decay=pick(decays, places),
+                            lr_scales=pick(scales, places), master=master and ptype != torch.float32, device_steps=True, **kw)
+                      for (ptype, _), places in kinds.items()]
+        self.max_norm = max_norm
+        first = self.parts[0]
+        first._args.max_norm = math.inf if max_norm is None else max_norm
+        self._dev, self.norm = first._dev, first.norm               # the one count, norm and factor of all parts
+        counts = [part._table.layout.partials for part in self.parts]
+        self._partials = torch.zeros(sum(counts), dtype=torch.float64, device=self._dev.device)
+        at = [sum(counts[:k]) for k in range(len(counts))]
+        self._partials_ptrs = [C.c_void_p(self._partials.data_ptr() + 8 * a) for a in at]
+        for part in self.parts:
+            part._table.also += [self._dev, self._partials]
+        self._table = first._table
+        torch.cuda.current_stream(self._dev.device).synchronize()      # cleared, for whichever stream comes first
+
+    @property
+    def lr(self):
+        return self.parts[0].lr
+
+    @lr.setter
+    def lr(self, lr):
+        for part in self.parts:
+            part.lr = lr
+
+    @property
+    def t(self) -> int:
+        """Number of steps taken (waits for the device)."""
+        return self.parts[0].t
+
+    @t.setter
+    def t(self, t: int):
+        self.parts[0].t = t
+
+    @property
+    def skipped(self) -> int:
+        """Steps left out because their norm was not finite (waits for the device)."""
+        return self.parts[0].skipped
+
+    def moments(self):
+        """(m, v) of every tensor as float32 copies, in the parameters' order."""
+        out = {}
+        for places, part in zip(self.places, self.parts):
+            out.update(zip(places, part.moments()))
+        return [out[k] for k in sorted(out)]
+
+    def state_dict(self) -> dict:
+        return {"parts": [part.state_dict() for part in self.parts]}
+
+    def load_state_dict(self, d: dict):
+        if len(d["parts"]) != len(self.parts):
+            raise ValueError("state_dict: of another number of parts")
+        for part, s in zip(self.parts, d["parts"]):
+            part.load_state_dict(s)
+
+    @_on_device
+    def step(self, grads: Optional[Sequence[torch.Tensor]] = None):
+        """One step on every tensor.  ``grads``: None, or tensors of the same sizes and types to take instead, from now on."""
+        if grads is not None and len(grads) != sum(len(places) for places in self.places):
+            raise ValueError("gradients: one per parameter")
+        was = [part._table.grads for part in self.parts]
+        try:
+            for places, part in zip(self.places, self.parts):
+                stream = part._table.ready(None if grads is None else [grads[k] for k in places])
+        except Exception:
+            if grads is not None:                                   # refused gradients are not kept, by any part
+                for part, g in zip(self.parts, was):
+                    part._table.ready(g)
+            raise
+        first, partials = self.parts[0], None
+        if self.max_norm is not None:
+            partials = self._partials_ptrs[0]
+            for part, at in zip(self.parts, self._partials_ptrs):
+                t = part._table
+                B._chk(B._lib.co3_grad_sumsq(t.layout_ref, t.plan_ptr, at, stream), "co3_grad_sumsq")
+        B._chk(B._lib.co3_step_begin(first._args_ref, partials, self._partials.numel(), first._lr_ptr, first._dev_ptr, stream),
+               "co3_step_begin")
+        for part in self.parts:
+            t = part._table
+            B._chk(part._step_fn(t.layout_ref, t.plan_ptr, part._master_ptr, *part._state_ptrs, part._args_ref, first._dev_ptr, stream),
+                   "co3_adamw")
+            torch.autograd.graph.increment_version(t.params)

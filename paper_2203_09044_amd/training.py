@@ -27,7 +27,7 @@ from co3_inputs import group_small_tensors, seg_offsets
 
 from . import binding as B
 from .binding import Fmt
-from .optim import AdamW, GradNorm
+from .optim import AdamW, GradNorm, MixedAdamW
 from .pipeline import Co3Pipeline
 
 
@@ -168,8 +168,8 @@ class Co3SGD:
 class Co3AdamW(Co3SGD):
     """Algorithm 1 with AdamW as the parameter server's update: the averaged reconstruction steps all tensors of the model in
     one pass, clipped by its global norm where ``max_norm`` is given, with states in 32 bits or in 8 (``optim.AdamW``).  Tensors of
-    one dimension (biases, scales of norms) are not decayed unless ``decay_vectors``.  16-bit models get 32-bit masters.  The
-    other arguments are those of ``Co3SGD``."""
+    one dimension (biases, scales of norms) are not decayed unless ``decay_vectors``.  16-bit parameters get 32-bit masters; a
+    model may mix types.  The other arguments are those of ``Co3SGD``."""
 
     def __init__(self, model: torch.nn.Module, users: int, fmt: Fmt, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.01, state_bits: int = 32, max_norm: Optional[float] = None, seed: int = 0,
@@ -177,8 +177,10 @@ class Co3AdamW(Co3SGD):
         super().__init__(model, users, fmt, lr, **codec)
         self._stepped = self.pipe.avg                     # the average whose segments the optimiser holds
         decays = [weight_decay if decay_vectors or p.dim() > 1 else 0.0 for p in self.params]
-        self.opt = AdamW(self.params, self._segments(self.pipe.avg), lr=lr, betas=betas, eps=eps, weight_decay=decays,
-                         state_bits=state_bits, master=self.params[0].dtype != torch.float32, max_norm=max_norm, seed=seed)
+        types = {p.dtype for p in self.params}
+        self.opt = (AdamW if len(types) == 1 else MixedAdamW)(
+            self.params, self._segments(self.pipe.avg), lr=lr, betas=betas, eps=eps, weight_decay=decays, state_bits=state_bits,
+            master=types != {torch.float32}, max_norm=max_norm, seed=seed)
 
     def _segments(self, avg: torch.Tensor):
         return [avg[a:b] for a, b in zip(self.seg_off[:-1], self.seg_off[1:])]

@@ -655,6 +655,100 @@ def test_offsets_beyond_32_bits(co3, bits, ptype, n):
 
 
 # ---- the framework's own path ---------------------------------------------------------------------------------------
+def mixed_case(bits, max_norm, **kw):
+    """The same parameters and gradients for a MixedAdamW and for one AdamW per type."""
+    torch.manual_seed(13)
+    types = [F32, BF16, F32, F16, BF16, F32]
+    params = [torch.randn(n, device="cuda").to(t) for n, t in zip((3000, 5000, 1, 300, 64, 0), types)]
+    grads = [torch.randn_like(p) for p in params]
+    decays = [0.1 * k for k in range(len(types))]
+    return types, params, grads, decays, dict(lr=1e-2, weight_decay=decays, state_bits=bits, master=True, max_norm=max_norm, seed=17, **kw)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("max_norm", [None, 0.5])
+def test_parameters_of_several_types_make_one_step(co3, bits, max_norm):
+    types, params, grads, decays, kw = mixed_case(bits, max_norm)
+    apart = [p.clone() for p in params]
+    opt = co3.MixedAdamW(params, grads, **kw)
+    assert sorted(k for places in opt.places for k in places) == list(range(len(types))) and len(opt.parts) == 3
+    # each part alone, with the factor of the common norm as what multiplies its gradients
+    alone = []
+    for places, part in zip(opt.places, opt.parts):
+        alone.append(co3.AdamW([apart[k] for k in places], [grads[k] for k in places], lr=1e-2, weight_decay=[decays[k] for k in places],
+                               state_bits=bits, master=types[places[0]] != F32, seed=17))
+    for t in range(3):
+        for g in grads:
+            g.copy_(torch.randn_like(g))
+        if t == 2:
+            grads = [g.clone() for g in grads]             # other tensors of the same types
+        opt.step(grads if t == 2 else None)
+        norm, c = O.norm([g.double().cpu().numpy() for g in grads], 1.0, max_norm or math.inf)
+        if max_norm is not None:
+            assert abs(float(opt.norm[0]) - norm) <= U * (1 + 1e-6) * norm and abs(float(opt.norm[1]) - c) <= U * (1 + 1e-6) * c
+        for places, one in zip(opt.places, alone):
+            one._args.grad_scale = float(opt.norm[1])
+            one.step([grads[k] for k in places])
+        assert opt.t == t + 1
+        for a, b in zip(params, apart):
+            assert torch.equal(a, b)
+        for part, one in zip(opt.parts, alone):
+            for a, b in zip(part._named().values(), one._named().values()):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    saved = opt.state_dict()
+    again = co3.MixedAdamW([p.clone() for p in params], grads, **kw)
+    again.load_state_dict(saved)
+    opt.lr = again.lr = 1e-3
+    opt.step()
+    again.step()
+    assert all(torch.equal(a, b) for a, b in zip(params, [p for _, p in sorted((k, p) for places, part in zip(again.places, again.parts)
+                                                                               for k, p in zip(places, part._table.params))]))
+    assert again.t == 4 and len(opt.moments()) == len(types)
+    assert all(m.shape == p.shape and v.shape == p.shape for (m, v), p in zip(opt.moments(), params))
+    if max_norm is not None:
+        keep = [p.clone() for p in params]
+        grads[1][3] = math.nan
+        opt.step()
+        assert opt.t == 4 and opt.skipped == 1 and all(torch.equal(a, b) for a, b in zip(params, keep))
+
+
+def test_a_captured_step_of_several_types(co3):
+    runs = []
+    for captured in (False, True):
+        _, params, grads, _, kw = mixed_case(8, 1.0)
+        opt = co3.MixedAdamW(params, grads, **kw)
+        if captured:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                opt.step()
+        for t in range(4):
+            for k, g in enumerate(grads):
+                g.fill_(0.01 * (t + k + 1))
+            graph.replay() if captured else opt.step()
+            torch.cuda.synchronize()
+            assert torch.rand(1 << 20, device="cuda").sum().item() > 0 and opt.t == t + 1
+        runs.append(params + [x.view(torch.uint8) for part in opt.parts for x in part._named().values()])
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+def test_mixed_refusals(co3):
+    x, y = torch.zeros(8, device="cuda"), torch.zeros(8, device="cuda").half()
+    for params, grads, kw in (([], [], {}), ([x, y], [x.clone()], {}), ([x, x], [x.clone(), x.clone()], {}), ([x], [x], {}),
+                              ([x, y.double()], [x.clone(), y.clone()], {}), ([x, y.cpu()], [x.clone(), y.cpu()], {}),
+                              ([x, y], [x.clone(), y.clone()], dict(max_norm=0.0)), ([x, y], [x.clone(), y.clone()], dict(weight_decay=[0.1]))):
+        with pytest.raises(ValueError):
+            co3.MixedAdamW(params, grads, **kw)
+    with pytest.raises(ValueError):                     # one parameter under two gradient types
+        co3.MixedAdamW([x, x], [x.clone(), x.clone().half()])
+    opt = co3.MixedAdamW([x, y], [torch.ones_like(x), torch.ones_like(y)], weight_decay=0.0, lr=0.5, device_steps=False)
+    for bad in ([x.clone()], [x.clone(), y.clone()[:4]], [x.clone() + 2, y]):
+        with pytest.raises(ValueError):
+            opt.step(bad)
+    assert opt.t == 0 and not x.any() and not y.any()
+    opt.step()                                          # with the gradients it was made with
+    assert opt.t == 1 and torch.allclose(x, torch.full_like(x, -0.5)) and torch.allclose(y, torch.full_like(y, -0.5))
+
+
 def problem(dtype=F32):
     torch.manual_seed(12)
     model = torch.nn.Sequential(torch.nn.Linear(48, 300), torch.nn.ReLU(), torch.nn.Linear(300, 10)).cuda().to(dtype)
@@ -691,6 +785,27 @@ def test_training_steps_the_model_with_the_averaged_reconstruction(co3, bits, ma
             assert abs(factor - c) <= U * (1 + 1e-6) * c
         check_step(opt.opt, sizes, before, [p.detach().reshape(-1).float().cpu().numpy() for p in opt.params], grads, w, t, factor, 1e-2,
                    (0.9, 0.999), 1e-8, decays, [1.0] * len(sizes), 21)
+    assert opt.opt.t == 3
+
+
+def test_training_a_model_of_several_types(co3):
+    """A 16-bit model with a 32-bit layer: masters for the one, the other itself, one norm over both."""
+    model, sample = problem(BF16)
+    model[2].to(F32)
+    loss = lambda x, c: torch.nn.functional.cross_entropy(x.float(), c)  # noqa: E731
+    cast = torch.nn.Sequential(model[0], model[1])
+    net = torch.nn.Module()
+    net.first, net.last = cast, model[2]
+    net.forward = lambda x: net.last(net.first(x).float())
+    opt = co3.Co3AdamW(net, 2, co3.Fmt(4, 3), lr=1e-2, state_bits=8, max_norm=0.5)
+    assert {p.dtype for p in opt.params} == {F32, BF16} and isinstance(opt.opt, co3.MixedAdamW)
+    for t in range(3):
+        masters = [x.clone() for part in opt.opt.parts for x in ([part.master] if part.master is not None else [])]
+        before = [p.detach().clone() for p in opt.params]
+        opt.step([sample(t, u) for u in range(2)], loss)
+        norm, c = O.norm([opt.pipe.avg[:opt.n].double().cpu().numpy()], 1.0, 0.5)
+        assert abs(float(opt.opt.norm[0]) - norm) <= U * (1 + 1e-6) * norm and abs(float(opt.opt.norm[1]) - c) <= U * (1 + 1e-6) * c
+        assert len(masters) == 1 and not any(torch.equal(p.detach(), b) for p, b in zip(opt.params, before))
     assert opt.opt.t == 3
 
 
