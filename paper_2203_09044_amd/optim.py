@@ -85,7 +85,9 @@ class _Table:
         self.device = self.grads[0].device
         self.lr_scales, self.weight_decays = _per_tensor(lr_scales, T, "lr_scales"), _per_tensor(weight_decays, T, "weight_decay")
         self._captured = []                      # plans that a captured graph goes on reading
-        self.also = []                           # memory of the handle that its launches use
+        self.also = []                           # memory of the handle that its launches use, made on the stream that is current now
+        with torch.cuda.device(self.device):
+            self._streams = {_raw_stream(self.device.index)}
         self._make()
 
     def _take(self, grads: Sequence[torch.Tensor]):
@@ -124,7 +126,9 @@ class _Table:
             raise ValueError("a parameter shares memory with another one or with a gradient") from e
         with torch.cuda.device(self.device):
             self.plan = host.to(self.device)
-            self._streams = {_raw_stream(self.device.index)}     # streams that the memory is known to
+            # the streams that all of the memory is known to: the plan to this one alone, `also` to those it was known to before
+            raw = _raw_stream(self.device.index)
+            self._streams = {raw} & self._streams
         self.layout, self.layout_ref, self.plan_ptr = layout, C.byref(layout), C.c_void_p(self.plan.data_ptr())
         self._watched, self._at, self._places = watched, at, list(range(len(at)))     # what the plan is for
         self._dtype = self.grads[0].dtype

@@ -1,0 +1,82 @@
+"""What the handles of the server's update keep and look at on the host (CPU): streams, the device's state and the launches are
+stand-ins that write down what they are asked for; sizes, plans and refusals are the library's own."""
+import contextlib
+
+import pytest
+import torch
+
+LAUNCHES = ("co3_grad_sumsq", "co3_grad_norm", "co3_step_begin", "co3_adamw", "co3_adamw8", "co3_adamw_clipped", "co3_adamw8_clipped")
+
+
+class Host:
+    """The machine as the handles see it: the current stream, whether it is being captured, what was launched and recorded."""
+
+    def __init__(self, lib):
+        self.stream, self.capturing, self.launched, self.recorded, self.lib = 1, False, [], [], lib
+
+    def synchronize(self):
+        pass
+
+    def __getattr__(self, name):                         # the library: launches are written down, the host side is its own
+        if name in LAUNCHES:
+            return lambda *a: self.launched.append(name) or 0
+        return getattr(self.lib, name)
+
+    def known_to(self, t):
+        return {s for kept, s in self.recorded if kept is t}
+
+
+@pytest.fixture
+def host(monkeypatch):
+    from paper_2203_09044_amd import binding, optim
+    h = Host(binding._lib)
+    monkeypatch.setattr(binding, "_lib", h)
+    monkeypatch.setattr(optim, "_raw_stream", lambda index: h.stream)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: h.capturing)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: h)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: None)
+    monkeypatch.setattr(torch.cuda, "device", lambda device: contextlib.nullcontext())
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: h.recorded.append((t, h.stream)))
+    return h
+
+
+def make(kind, sizes=(300, 5), **kw):
+    """A handle, and the list of what its launches use beside the plan."""
+    from paper_2203_09044_amd import AdamW, GradNorm, MixedAdamW
+    if kind == "norm":
+        opt = GradNorm([torch.zeros(n) for n in sizes])
+        return opt, opt.compute, opt._table.also
+    params = [torch.zeros(n) for n in sizes]
+    if kind == "mixed":
+        params[1] = params[1].half()
+        opt = MixedAdamW(params, [torch.zeros_like(p) for p in params], max_norm=1.0, **kw)
+        return opt, opt.step, [t for part in opt.parts for t in part._table.also]
+    opt = AdamW(params, [torch.zeros_like(p) for p in params], state_bits=8, max_norm=1.0, **kw)
+    return opt, opt.step, opt._table.also
+
+
+def new_gradients(opt):
+    tables = [part._table for part in getattr(opt, "parts", [])] or [opt._table]
+    places = getattr(opt, "places", [list(range(len(tables[0].grads)))])
+    by_place = {k: torch.zeros_like(g) for ks, t in zip(places, tables) for k, g in zip(ks, t.grads)}
+    return [by_place[k] for k in sorted(by_place)]
+
+
+@pytest.mark.parametrize("kind", ["norm", "step", "mixed"])
+def test_memory_is_known_to_a_stream_that_makes_a_new_plan(host, kind):
+    """The handle's memory belongs to the stream it was made on.  A call on another stream makes it known there, also where that
+    call makes a new plan (whose own memory belongs to the stream of that call); else it could be given away under the call."""
+    opt, call, memory = make(kind)
+    call()
+    assert not host.recorded
+    for stream in (2, 3):
+        host.stream = stream
+        call(new_gradients(opt))
+        assert all(stream in host.known_to(t) for t in memory)
+        call(new_gradients(opt))
+        call()
+    host.stream = 1                                       # back: the last plan belongs to stream 3
+    call()
+    tables = [part._table for part in getattr(opt, "parts", [])] or [opt._table]
+    assert all(1 in host.known_to(t.plan) for t in tables)
