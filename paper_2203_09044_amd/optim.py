@@ -84,7 +84,8 @@ class _Table:
         T = len(self.grads)
         self.device = self.grads[0].device
         self.lr_scales, self.weight_decays = _per_tensor(lr_scales, T, "lr_scales"), _per_tensor(weight_decays, T, "weight_decay")
-        self._captured = []                      # plans that a captured graph goes on reading
+        self._captured = []                      # plans and learning rates that a captured graph goes on reading
+        self.lr = None                           # the learning rate, where it lies on the device
         self.also = []                           # memory of the handle that its launches use, made on the stream that is current now
         with torch.cuda.device(self.device):
             self._streams = {_raw_stream(self.device.index)}
@@ -155,11 +156,11 @@ class _Table:
                 raise
         raw = _raw_stream(self.device.index)
         if capturing:
-            if not any(p is self.plan for p in self._captured):
-                self._captured.append(self.plan)
+            if not any(plan is self.plan and lr is self.lr for plan, lr in self._captured):
+                self._captured.append((self.plan, self.lr))
         elif raw not in self._streams:
             self._streams.add(raw)
-            for t in [self.plan] + self.also:
+            for t in [self.plan] + self.also + ([] if self.lr is None else [self.lr]):
                 t.record_stream(torch.cuda.current_stream(self.device))
         return C.c_void_p(raw)
 
@@ -220,7 +221,8 @@ class AdamW:
     device_steps    the device counts the steps, which a captured step needs (always so with max_norm or a tensor ``lr``)
 
     The state arrays hold the tensors one behind another: packed with 32 bits, each from a multiple of 256 on with 8.  They stay the
-    handle's: a program copies into them.  A graph that holds a captured step needs the handle alive.
+    handle's: a program copies into them.  A graph that holds a captured step needs the handle alive, and the parameters and
+    gradients that it was captured with; a learning rate on the device the handle keeps for it.
     """
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: Union[float, torch.Tensor] = 1e-3,
@@ -287,11 +289,13 @@ class AdamW:
                 self._device_steps = True
             self._args.lr = 0.0
             self._lr_ptr = C.c_void_p(lr.data_ptr())
+            if lr is not self._table.lr:
+                self._table.lr, self._table._streams = lr, set()      # known to no stream yet
         elif not (lr >= 0.0 and math.isfinite(lr)):
             raise ValueError("lr must be finite and not negative")
         else:
             self._args.lr = float(lr)
-            self._lr_ptr = None
+            self._lr_ptr = self._table.lr = None
         self._lr = lr
 
     @property

@@ -60,3 +60,24 @@ def test_a_handle_dropped_behind_a_step_with_a_new_plan_on_another_stream(co3, k
     junk = [torch.full((n,), math.nan, device="cuda") for n in (1_000_080, 2_000_000, 250_020, 7_816, 64, 16) for _ in range(8)]
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, got)) and junk
+
+
+def test_replays_read_the_learning_rate_of_their_capture(co3):
+    p, g = torch.randn(5000, device="cuda"), torch.randn(5000, device="cuda")
+    want = p.clone()
+    opt = co3.AdamW([p], [g], lr=torch.tensor([1e-2], device="cuda"), max_norm=1.0)
+    ref = co3.AdamW([want], [g], lr=torch.tensor([1e-2], device="cuda"), max_norm=1.0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step()
+    for t in range(3):
+        opt.lr = torch.tensor([1e-3 * (t + 1)], device="cuda") if t < 2 else 5e-3     # the captured one has no other owner
+        junk = [torch.full((1,), math.nan, device="cuda") for _ in range(256)]
+        graph.replay()
+        ref.lr = torch.tensor([1e-2], device="cuda")
+        ref.step()
+        opt.step()
+        ref.lr = opt.lr
+        ref.step()
+        torch.cuda.synchronize()
+        assert torch.equal(p, want) and opt.t == ref.t == 2 * t + 2 and junk

@@ -1,6 +1,8 @@
 """What the handles of the server's update keep and look at on the host (CPU): streams, the device's state and the launches are
 stand-ins that write down what they are asked for; sizes, plans and refusals are the library's own."""
 import contextlib
+import gc
+import weakref
 
 import pytest
 import torch
@@ -80,3 +82,40 @@ def test_memory_is_known_to_a_stream_that_makes_a_new_plan(host, kind):
     call()
     tables = [part._table for part in getattr(opt, "parts", [])] or [opt._table]
     assert all(1 in host.known_to(t.plan) for t in tables)
+
+
+def gone(refs):
+    gc.collect()
+    return [r() is None for r in refs]
+
+
+@pytest.mark.parametrize("kind", ["step", "mixed"])
+def test_a_captured_step_keeps_the_learning_rate_that_it_reads(host, kind):
+    """A graph reads the device float that was the learning rate at its capture, at every replay: the handle keeps it when it gets
+    another one.  One that no graph reads is not kept, and is known to the streams that it was used on."""
+    opt, call, _ = make(kind, lr=torch.tensor([1e-3]))
+    host.capturing = True
+    call()
+    host.capturing = False
+    refs = [weakref.ref(opt.lr)]
+    opt.lr = torch.tensor([2e-3])
+    refs.append(weakref.ref(opt.lr))
+    host.stream = 2
+    call()
+    assert 2 in host.known_to(opt.lr)
+    host.recorded.clear()
+    opt.lr = torch.tensor([3e-3])
+    call()
+    assert 2 in host.known_to(opt.lr)
+    host.recorded.clear()
+    opt.lr = 1e-3
+    call()
+    assert not host.recorded and gone(refs) == [False, True]
+
+
+def test_a_plan_and_a_rate_that_were_captured_are_kept_once(host):
+    opt, call, _ = make("step", lr=torch.tensor([1e-3]))
+    host.capturing = True
+    for _ in range(5):
+        call()
+    assert len(opt._table._captured) == 1
