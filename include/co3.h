@@ -482,9 +482,10 @@ int32_t co3_step_plan(const co3_step_tensor *tensors_host, int32_t T, const co3_
                       size_t plan_bytes);
 
 /*
- * Sums of squares, in fp64, of the gradients of a plan: one launch.  partials [layout->partials] double, zeroed once by the caller; calls
- * that may run at the same time must not share them.  Several tables, as of models with parameters of several types,
- * write one behind another and are finished together by co3_step_begin.
+ * Sums of squares, in fp64, of the gradients of a plan: one launch.  partials: workspace of layout->partials doubles, zeroed once by
+ * the caller.  Tables of any sizes may take turns on one workspace; calls that may run at the same time must not share it, and a
+ * workspace that begins inside another one is zeroed again before co3_grad_norm or a clipped step takes it.  Several tables, as of
+ * models with parameters of several types, write one behind another and are finished together by co3_step_begin.
  */
 int32_t co3_grad_sumsq(const co3_step_layout *layout_host, const void *plan, double *partials, void *stream);
 

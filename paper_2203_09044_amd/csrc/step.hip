@@ -172,11 +172,12 @@ __device__ __forceinline__ void finish_norm(double s, bool norm, const Co3StepFi
     f.dev->var = next->var;
 }
 
-// partials[workgroup] = sum of the squares of its pieces; a wavefront takes a piece, ROUNDS vectors of it in flight.  In 64 bits: the
+// partials[1 + workgroup] = sum of the squares of its pieces; a wavefront takes a piece, ROUNDS vectors of it in flight.  In 64 bits: the
 // squares of 24-bit numbers are exact and none overflows, so the norm is right for any finite gradient; the sums are
 // taken in a fixed order, so it is the same in every run.  Where something is to be made of the sums, the workgroup
 // that is the last to have written its own does it: that saves a launch (65,536 elements: 5.5 us a call, with a second
-// kernel 10.7); the ticket behind the partial sums (zero between calls) says which one it is.  Tickets are drawn one
+// kernel 10.7); the ticket in front of the partial sums (zero between calls, so at the same place however many sums a table has: tables
+// may take turns on a workspace) says which one it is.  Tickets are drawn one
 // after another, some 8 ns each, so few large workgroups are better than many: one of 16 wavefronts to a compute unit reads 100 M
 // bf16 elements in 33.2 us (6.0 TB/s, bound by the reading), 512 of them in 36.3, 2048 of four wavefronts in 52.3.
 template <int G, bool NT>
@@ -211,22 +212,25 @@ __global__ __launch_bounds__(ST_NORM_BLOCK) void k_grad_sumsq(const Co3StepChunk
     }
     const double t = block_sum_f64((s[0] + s[1]) + (s[2] + s[3]), red);
     if (!f.out && !f.dev) {
-        if (threadIdx.x == 0) partials[blockIdx.x] = t;
+        if (threadIdx.x == 0) {
+            partials[1 + blockIdx.x] = t;
+            if (blockIdx.x == 0) partials[0] = 0.0;      // no ticket here, and nothing to the sum
+        }
         return;
     }
     if (threadIdx.x == 0) {
         // The sum is written through to where every compute unit sees it, and has arrived there before the ticket is drawn; a
         // release would write back the whole of the L2 first (2048 of them: 78 us).  The last ticket sets the counter back.
-        __hip_atomic_store(partials + blockIdx.x, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(partials + 1 + blockIdx.x, t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        ticket = atomicInc(reinterpret_cast<uint32_t *>(partials + gridDim.x), gridDim.x - 1);
+        ticket = atomicInc(reinterpret_cast<uint32_t *>(partials), gridDim.x - 1);
     }
     __syncthreads();
     if (ticket != gridDim.x - 1) return;
     prepare_next(f, &next);
     double all = 0.0;
     for (uint32_t i = threadIdx.x; i < gridDim.x; i += ST_NORM_BLOCK)
-        all += __hip_atomic_load(partials + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        all += __hip_atomic_load(partials + 1 + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     all = block_sum_f64(all, red);
     if (threadIdx.x == 0) finish_norm(all, true, f, &next);
 }

@@ -81,3 +81,40 @@ def test_replays_read_the_learning_rate_of_their_capture(co3):
         ref.step()
         torch.cuda.synchronize()
         assert torch.equal(p, want) and opt.t == ref.t == 2 * t + 2 and junk
+
+
+def norms(co3, sizes, dtype=F32):
+    """Tables for the C calls: gradients, layout, plan and the norm in float64 of every one."""
+    out = []
+    for k, n in enumerate(sizes):
+        g = torch.from_numpy(np.random.default_rng(k).standard_normal(n).astype(np.float32) * (k + 1)).cuda().to(dtype)
+        t = co3.GradNorm([g])._table
+        out.append((g, t.layout, t.plan, O.norm([g.double().cpu().numpy()])[0]))
+    return out
+
+
+def test_tables_of_different_sizes_take_turns_on_one_workspace(co3):
+    """A workspace zeroed once serves one table after another, with as many partial sums as each of them has, whole norms and
+    sums that a step is begun with."""
+    B = co3.binding
+    tables = norms(co3, [3_000_000, 40_000, 700, 9_000_000, 1, 250_000])
+    assert len({L.partials for _, L, _, _ in tables}) >= 4
+    work = torch.zeros(sum(L.partials for _, L, _, _ in tables), dtype=torch.float64, device="cuda")
+    state = torch.zeros(64, dtype=torch.uint8, device="cuda")
+    args = B.AdamwArgs(1e-3, 0.9, 0.999, 1e-8, 1.0, 1.0, 0, 0)
+    near = lambda got, want: abs(float(got) - want) <= U * (1 + 1e-6) * want  # noqa: E731
+    for turn in range(2):
+        for order in (tables, tables[::-1]):
+            for _, layout, plan, want in order:
+                out = torch.full((2,), -7.0, device="cuda")
+                B.grad_norm(layout, plan, 1.0, 1.0, out, work)
+                assert near(out[0], want) and near(out[1], 1.0 / (want + 1e-6))
+            for first in range(len(order)):                       # one table's sums behind another's, begun where any of them was
+                some = order[first:first + 3]
+                at = 0
+                for _, layout, plan, _ in some:
+                    B.grad_sumsq(layout, plan, work[at:])
+                    at += layout.partials
+                B.step_begin(args, state, work[:at])
+                want = math.sqrt(sum(w * w for _, _, _, w in some))
+                assert near(state.view(torch.float32)[4], want)
