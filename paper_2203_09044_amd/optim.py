@@ -134,6 +134,15 @@ class _Table:
         self._watched, self._at, self._places = watched, at, list(range(len(at)))     # what the plan is for
         self._dtype = self.grads[0].dtype
 
+    def now(self):
+        """Gradients and plan as they are, for ``back``."""
+        return (self.grads, self.plan, self._streams, self.layout, self.layout_ref, self.plan_ptr, self._watched, self._at, self._places,
+                self._dtype)
+
+    def back(self, was):
+        (self.grads, self.plan, self._streams, self.layout, self.layout_ref, self.plan_ptr, self._watched, self._at, self._places,
+         self._dtype) = was
+
     def ready(self, grads: Optional[Sequence[torch.Tensor]], capturable: bool = True) -> C.c_void_p:
         """The plan is that of the tensors as they lie now; returns the current stream of their device, which is the current one."""
         capturing = torch.cuda.is_current_stream_capturing()
@@ -462,14 +471,18 @@ class MixedAdamW:
         """One step on every tensor.  ``grads``: None, or tensors of the same sizes and types to take instead, from now on."""
         if grads is not None and len(grads) != sum(len(places) for places in self.places):
             raise ValueError("gradients: one per parameter")
-        was = [part._table.grads for part in self.parts]
+        tables = [part._table for part in self.parts]
+        was = [t.now() for t in tables]
         try:
-            for places, part in zip(self.places, self.parts):
-                stream = part._table.ready(None if grads is None else [grads[k] for k in places])
+            for places, t in zip(self.places, tables):
+                stream = t.ready(None if grads is None else [grads[k] for k in places])
+            # a part's plan is checked against its own tensors: one that is new, against the other parts' too
+            if any(t.plan is not w[1] for t, w in zip(tables, was)) and _overlapping([p for t in tables for p in t.params],
+                                                                                     [g for t in tables for g in t.grads]):
+                raise ValueError("a parameter shares memory with another one or with a gradient")
         except Exception:
-            if grads is not None:                                   # refused gradients are not kept, by any part
-                for part, g in zip(self.parts, was):
-                    part._table.ready(g)
+            for t, w in zip(tables, was):                           # what was refused is not kept, by any part
+                t.back(w)
             raise
         first, partials = self.parts[0], None
         if self.max_norm is not None:

@@ -119,3 +119,46 @@ def test_a_plan_and_a_rate_that_were_captured_are_kept_once(host):
     for _ in range(5):
         call()
     assert len(opt._table._captured) == 1
+
+
+def two_types():
+    """Parameters of two types, 32 bytes each, with their gradients as a handle of two parts."""
+    from paper_2203_09044_amd import MixedAdamW
+    x, y = torch.nn.Parameter(torch.ones(8)), torch.nn.Parameter(torch.ones(16).half())
+    return x, y, MixedAdamW([x, y], [torch.ones(8), torch.ones(16).half()])
+
+
+def test_a_gradient_on_another_parts_parameter_is_refused(host):
+    """A part that is stepped first would change the other's gradient before that is read."""
+    x, y, opt = two_types()
+    opt.step()
+    before, launched = [part._table.grads[0] for part in opt.parts], len(host.launched)
+    for bad in ([y.detach().view(torch.float32), torch.ones(16).half()], [torch.ones(8), x.detach().view(torch.float16)],
+                [y.detach()[4:12].view(torch.float32).repeat(2), x.detach().view(torch.float16)]):
+        for _ in range(2):
+            with pytest.raises(ValueError):
+                opt.step(bad)
+            assert len(host.launched) == launched and all(part._table.grads[0] is g for part, g in zip(opt.parts, before))
+    host.capturing = True                                       # what was refused changed nothing: a capture needs no call before it
+    opt.step()
+    host.capturing = False
+    fine = [torch.ones(8), torch.ones(16).half()]
+    opt.step(fine)
+    assert len(host.launched) == launched + 6 and all(part._table.grads[0] is g for part, g in zip(opt.parts, fine))
+
+
+def test_a_parameter_moved_onto_another_parts_memory_is_refused(host):
+    x, y, opt = two_types()
+    opt.step()
+    own, launched = x.data, len(host.launched)
+    x.data = y.detach().view(torch.float32)
+    for _ in range(2):
+        with pytest.raises(ValueError):
+            opt.step()
+    x.data = opt.parts[1]._table.grads[0].view(torch.float32)   # a parameter on another part's gradient
+    with pytest.raises(ValueError):
+        opt.step()
+    assert len(host.launched) == launched
+    x.data = own
+    opt.step()
+    assert len(host.launched) == launched + 3
