@@ -16,19 +16,12 @@ import numpy as np
 import torch
 
 from . import binding as B
+from ._tensors import look as _look, same as _same
 
 PerTensor = Union[float, Sequence[float]]
 
 # the handle of a device's current stream without the object around it (0.1 us against 1.8)
 _raw_stream = torch._C._cuda_getCurrentRawStream
-
-
-def _same_addresses(tensors, addresses, places):
-    return [t.data_ptr() for t in tensors] == addresses
-
-
-# the same in one call where torch has it (28 ns a tensor against 42)
-_same_addresses = getattr(torch._C, "_tensors_data_ptrs_at_indices_equal", _same_addresses)
 
 
 def _per_tensor(x: PerTensor, T: int, what: str) -> List[float]:
@@ -73,8 +66,8 @@ def _overlapping(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor]) 
 
 
 class _Table:
-    """Plan of a list of tensors on their device.  The addresses are looked at before every use, and a new plan is made when
-    a tensor has moved."""
+    """Plan of a list of tensors on their device.  The tensors are looked at before every use (address, elements, type,
+    contiguity), and a new plan is made when one has moved or is of another type."""
 
     def __init__(self, params: Optional[Sequence[torch.Tensor]], grads: Sequence[torch.Tensor], state_bits: int,
                  lr_scales: PerTensor = 1.0, weight_decays: PerTensor = 0.0):
@@ -85,7 +78,8 @@ class _Table:
         self.device = self.grads[0].device
         self.lr_scales, self.weight_decays = _per_tensor(lr_scales, T, "lr_scales"), _per_tensor(weight_decays, T, "weight_decay")
         self._captured = []                      # plans and learning rates that a captured graph goes on reading
-        self.lr = None                           # the learning rate, where it lies on the device
+        self.lr = None                           # the learning rate and its memory, where it lies on the device
+        self.masters = False
         self.also = []                           # memory of the handle that its launches use, made on the stream that is current now
         with torch.cuda.device(self.device):
             self._streams = {_raw_stream(self.device.index)}
@@ -104,6 +98,8 @@ class _Table:
             _check_tensors(self.params, "parameters")
             if sizes != [p.numel() for p in self.params]:
                 raise ValueError("parameters: as many elements as before")
+            if getattr(self, "masters", False) and self.params[0].dtype == torch.float32:
+                raise ValueError("float32 parameters are their own masters")
             if grads[0].device != self.params[0].device:
                 raise ValueError("gradients: on the parameters' device")
         if sizes != [g.numel() for g in grads]:
@@ -112,7 +108,7 @@ class _Table:
     def _make(self):
         T = len(self.grads)
         watched = self.grads + (self.params or [])
-        at = [t.data_ptr() for t in watched]
+        seen, at = _look(watched), [t.data_ptr() for t in watched]
         table = np.zeros(T, dtype=[("param", "u8"), ("grad", "u8"), ("n", "i8"), ("lr_scale", "f4"), ("weight_decay", "f4")])
         if self.params is not None:
             table["param"] = at[T:]
@@ -131,17 +127,14 @@ class _Table:
             raw = _raw_stream(self.device.index)
             self._streams = {raw} & self._streams
         self.layout, self.layout_ref, self.plan_ptr = layout, C.byref(layout), C.c_void_p(self.plan.data_ptr())
-        self._watched, self._at, self._places = watched, at, list(range(len(at)))     # what the plan is for
-        self._dtype = self.grads[0].dtype
+        self._watched, self._seen = watched, seen                # what the plan is for
 
     def now(self):
         """Gradients and plan as they are, for ``back``."""
-        return (self.grads, self.plan, self._streams, self.layout, self.layout_ref, self.plan_ptr, self._watched, self._at, self._places,
-                self._dtype)
+        return self.grads, self.plan, self._streams, self.layout, self.layout_ref, self.plan_ptr, self._watched, self._seen
 
     def back(self, was):
-        (self.grads, self.plan, self._streams, self.layout, self.layout_ref, self.plan_ptr, self._watched, self._at, self._places,
-         self._dtype) = was
+        self.grads, self.plan, self._streams, self.layout, self.layout_ref, self.plan_ptr, self._watched, self._seen = was
 
     def ready(self, grads: Optional[Sequence[torch.Tensor]], capturable: bool = True) -> C.c_void_p:
         """The plan is that of the tensors as they lie now; returns the current stream of their device, which is the current one."""
@@ -152,10 +145,10 @@ class _Table:
         if grads is not None:
             self._take(grads)
             self._watched = self.grads + (self.params or [])
-        if not _same_addresses(self._watched, self._at, self._places) or self.grads[0].dtype != self._dtype:
+        if not _same(self._watched, self._seen):
             try:
                 if capturing:
-                    raise RuntimeError("a tensor has moved since the last call: call once before the capture")
+                    raise RuntimeError("a tensor has moved or changed since the last call: call once before the capture")
                 if grads is None:
                     self._check(self.grads)
                 self._make()
@@ -169,7 +162,7 @@ class _Table:
                 self._captured.append((self.plan, self.lr))
         elif raw not in self._streams:
             self._streams.add(raw)
-            for t in [self.plan] + self.also + ([] if self.lr is None else [self.lr]):
+            for t in [self.plan] + self.also + ([] if self.lr is None else [self.lr[0]]):
                 t.record_stream(torch.cuda.current_stream(self.device))
         return C.c_void_p(raw)
 
@@ -266,6 +259,7 @@ class AdamW:
         self.master = None
         if master:
             self.master = torch.zeros(n, dtype=torch.float32, **z)
+            t.masters = True
             self.take_masters()
         # an array of no elements has no address: any will do, none is read
         self._state_ptrs = [C.c_void_p(s.data_ptr() or t.plan.data_ptr()) for s in states]
@@ -279,6 +273,7 @@ class AdamW:
         self._partials = torch.zeros(t.layout.partials if max_norm is not None else 1, dtype=torch.float64, **z)
         self._partials_ptr = C.c_void_p(self._partials.data_ptr())
         self._device_steps = device_steps or max_norm is not None
+        self._lr_seen = None
         self.lr = lr
         t.also = [self._dev, self._partials, *self._named().values()]
         torch.cuda.current_stream(t.device).synchronize()      # cleared, for whichever stream comes first
@@ -297,15 +292,20 @@ class AdamW:
                 self._dev[0] = self._t
                 self._device_steps = True
             self._args.lr = 0.0
-            self._lr_ptr = C.c_void_p(lr.data_ptr())
-            if lr is not self._table.lr:
-                self._table.lr, self._table._streams = lr, set()      # known to no stream yet
+            seen = _look([lr])
+            if seen != self._lr_seen:
+                self._lr_seen, self._lr_ptr = seen, C.c_void_p(lr.data_ptr())
+                self._table.lr, self._table._streams = (lr, lr.untyped_storage()), set()      # known to no stream yet
         elif not (lr >= 0.0 and math.isfinite(lr)):
             raise ValueError("lr must be finite and not negative")
         else:
             self._args.lr = float(lr)
-            self._lr_ptr = self._table.lr = None
+            self._lr_seen = self._lr_ptr = self._table.lr = None
         self._lr = lr
+
+    def _look_at_lr(self):
+        if self._lr_seen is not None and not _same([self._lr], self._lr_seen):
+            self.lr = self._lr
 
     @property
     def t(self) -> int:
@@ -371,6 +371,7 @@ class AdamW:
     def step(self, grads: Optional[Sequence[torch.Tensor]] = None):
         """One step on every tensor.  ``grads``: None, or tensors of the same sizes to take instead, from now on."""
         t = self._table
+        self._look_at_lr()
         stream = t.ready(grads, self._device_steps)
         if self.max_norm is not None:
             B._chk(self._clipped_fn(t.layout_ref, t.plan_ptr, self._master_ptr, *self._state_ptrs, self._args_ref, self._lr_ptr,
@@ -471,6 +472,8 @@ class MixedAdamW:
         """One step on every tensor.  ``grads``: None, or tensors of the same sizes and types to take instead, from now on."""
         if grads is not None and len(grads) != sum(len(places) for places in self.places):
             raise ValueError("gradients: one per parameter")
+        for part in self.parts:
+            part._look_at_lr()
         tables = [part._table for part in self.parts]
         was = [t.now() for t in tables]
         try:

@@ -162,3 +162,92 @@ def test_a_parameter_moved_onto_another_parts_memory_is_refused(host):
     x.data = own
     opt.step()
     assert len(host.launched) == launched + 3
+
+
+def one_type(dtype=torch.float32, **kw):
+    from paper_2203_09044_amd import AdamW
+    p, g = torch.nn.Parameter(torch.ones(6, 6, dtype=dtype)), torch.ones(6, 6, dtype=dtype)
+    return p, g, AdamW([p], [g], **kw)
+
+
+CHANGES = {"shorter": lambda x: x[:3], "transposed": lambda x: x.t(), "strided": lambda x: x[:, ::2], "longer": lambda x: x.as_strided((6, 7), (7, 1)),
+           "of a type that has no step": lambda x: x.view(torch.int32)}
+
+
+@pytest.mark.parametrize("which,change", [(w, c) for w in ("parameter", "gradient") for c in CHANGES if w == "gradient" or "type" not in c])
+def test_a_tensor_that_is_another_one_at_the_same_address_is_refused(host, which, change):
+    """What the tensor is goes with where it lies: the plan would go on with the elements, their order or their type from before."""
+    p, g, opt = one_type()
+    room = torch.ones(50)
+    p.data, g.data = room[:36].view(6, 6), room.clone()[:36].view(6, 6)
+    opt.step()
+    x = p if which == "parameter" else g
+    was = x.data
+    x.data = CHANGES[change](was)
+    assert x.data_ptr() == was.data_ptr()
+    for _ in range(2):
+        with pytest.raises(ValueError):
+            opt.step()
+    host.capturing = True
+    with pytest.raises((RuntimeError, ValueError)):
+        opt.step()
+    host.capturing = False
+    assert host.launched == ["co3_adamw"] and opt.t == 1
+    x.data = was
+    opt.step()
+    assert host.launched == ["co3_adamw"] * 2
+
+
+def test_a_norms_gradient_that_became_shorter_is_refused(host):
+    from paper_2203_09044_amd import GradNorm
+    g = torch.ones(10)
+    norm = GradNorm([g])
+    norm.compute()
+    g.data = g.data[:4]
+    with pytest.raises(ValueError):
+        norm.compute()
+    assert host.launched == ["co3_grad_norm"]
+
+
+def test_a_parameter_of_another_type_at_the_same_address_has_a_plan_of_its_type(host):
+    """16-bit types may change: the next step is that of the new one, as where a tensor moves."""
+    p, g, opt = one_type(torch.bfloat16)
+    opt.step()
+    assert (opt._table.layout.param_type, opt._table.layout.grad_type) == (1, 1)
+    p.data = p.data.view(torch.float16)
+    opt.step()
+    assert (opt._table.layout.param_type, opt._table.layout.grad_type) == (2, 1)
+    p.data = p.data.view(torch.bfloat16)
+    opt.step([g])                                             # with gradients given, too
+    assert (opt._table.layout.param_type, opt._table.layout.grad_type) == (1, 1)
+    g.data = g.data.view(torch.float16)
+    opt.step()
+    assert (opt._table.layout.param_type, opt._table.layout.grad_type) == (1, 2)
+
+
+def test_parameters_that_became_their_own_masters_are_refused(host):
+    p, g, opt = one_type(torch.bfloat16, master=True)
+    opt.step()
+    p.data = p.data.float()
+    for grads in (None, [g]):
+        with pytest.raises(ValueError):
+            opt.step(grads)
+    assert host.launched == ["co3_adamw"]
+
+
+@pytest.mark.parametrize("kind", ["step", "mixed"])
+def test_a_learning_rate_that_moved_is_read_where_it_lies(host, kind):
+    lr = torch.tensor([1e-3])
+    opt, call, _ = make(kind, lr=lr)
+    parts = getattr(opt, "parts", [opt])
+    host.capturing = True
+    call()
+    host.capturing = False
+    storage = weakref.ref(lr.untyped_storage())
+    lr.data = torch.tensor([2e-3])
+    call()
+    assert all(part._lr_ptr.value == lr.data_ptr() for part in parts) and gone([storage]) == [False]
+    for bad in (torch.ones(2), torch.ones(1).half()):
+        lr.data = bad
+        with pytest.raises(ValueError):
+            call()
