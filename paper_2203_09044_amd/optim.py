@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import math
+import operator
 from typing import List, Optional, Sequence, Union
 
 import numpy as np
@@ -355,14 +356,22 @@ class AdamW:
     def state_dict(self) -> dict:
         return {"t": self.t, "skipped": self.skipped, "seed": int(self._args.seed), **{k: v.clone() for k, v in self._named().items()}}
 
-    def load_state_dict(self, d: dict):
-        named = self._named()
-        for k, v in named.items():
-            if k not in d or d[k].dtype != v.dtype or d[k].shape != v.shape:
+    def _check_state(self, d: dict):
+        if not isinstance(d, dict):
+            raise ValueError("state_dict: a dict is needed")
+        for k, v in self._named().items():
+            if not isinstance(d.get(k), torch.Tensor) or d[k].dtype != v.dtype or d[k].shape != v.shape:
                 raise ValueError(f"state_dict: {k} is missing or of another type or size")
-        for k, v in named.items():
+        for k in ("t", "skipped", "seed"):
+            if not hasattr(d.get(k), "__index__") or operator.index(d[k]) < 0:
+                raise ValueError(f"state_dict: {k} is missing or not a whole number from 0")
+
+    def load_state_dict(self, d: dict):
+        """All of a state, or, where some of it is missing or does not fit, nothing (ValueError)."""
+        self._check_state(d)
+        for k, v in self._named().items():
             v.copy_(d[k])
-        self._args.seed = d["seed"]
+        self._args.seed = operator.index(d["seed"])
         self.t = d["t"]
         self._dev[1] = d["skipped"]
 
@@ -462,8 +471,11 @@ class MixedAdamW:
         return {"parts": [part.state_dict() for part in self.parts]}
 
     def load_state_dict(self, d: dict):
-        if len(d["parts"]) != len(self.parts):
+        """All of a state, or, where some of it is missing or does not fit, nothing (ValueError)."""
+        if not isinstance(d.get("parts"), (list, tuple)) or len(d["parts"]) != len(self.parts):
             raise ValueError("state_dict: of another number of parts")
+        for part, s in zip(self.parts, d["parts"]):
+            part._check_state(s)
         for part, s in zip(self.parts, d["parts"]):
             part.load_state_dict(s)
 

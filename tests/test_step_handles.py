@@ -251,3 +251,50 @@ def test_a_learning_rate_that_moved_is_read_where_it_lies(host, kind):
         lr.data = bad
         with pytest.raises(ValueError):
             call()
+
+
+def contents(opt):
+    parts = getattr(opt, "parts", [opt])
+    return [x.view(torch.uint8).clone() for part in parts for x in list(part._named().values()) + [part._dev]] + [
+        torch.tensor([part._args.seed, part._t]) for part in parts]
+
+
+@pytest.mark.parametrize("kind", ["step", "mixed"])
+@pytest.mark.parametrize("fault", ["array missing", "array short", "array of another type", "no seed", "no count", "count below zero", "no skipped", "no state"])
+def test_a_state_that_is_refused_changes_nothing(host, kind, fault):
+    """The last array of the last part is the one that does not fit, or a number is missing: nothing of the others is loaded."""
+    opt, _, _ = make(kind, seed=3)
+    other, _, _ = make(kind, seed=4)
+    for part in getattr(other, "parts", [other]):
+        for x in part._named().values():
+            x.view(torch.uint8).fill_(17)
+        part.t = 5
+    saved = other.state_dict()
+    last = saved["parts"][-1] if kind == "mixed" else saved
+    name = list((getattr(other, "parts", [other])[-1])._named())[-1]
+    if fault == "array missing":
+        del last[name]
+    elif fault == "array short":
+        last[name] = last[name][1:]
+    elif fault == "array of another type":
+        last[name] = last[name].float().double()
+    elif fault == "count below zero":
+        last["t"] = -1
+    elif fault == "no state":
+        saved = {"parts": saved["parts"][:-1] + [None]} if kind == "mixed" else {}
+    else:
+        del last[{"no seed": "seed", "no count": "t", "no skipped": "skipped"}[fault]]
+    before = contents(opt)
+    with pytest.raises(ValueError):
+        opt.load_state_dict(saved)
+    assert all(torch.equal(a, b) for a, b in zip(before, contents(opt)))
+    opt.load_state_dict(other.state_dict())
+    assert all(torch.equal(a, b) for a, b in zip(contents(other), contents(opt))) and opt.t == 5
+
+
+def test_a_state_of_parts_goes_to_parts(host):
+    step, _, _ = make("step")
+    mixed, _, _ = make("mixed")
+    for opt, saved in ((mixed, step.state_dict()), (mixed, {"parts": [step.state_dict()]}), (step, mixed.state_dict())):
+        with pytest.raises(ValueError):
+            opt.load_state_dict(saved)
