@@ -460,6 +460,11 @@ class MixedAdamW:
         """Steps left out because their norm was not finite (waits for the device)."""
         return self.parts[0].skipped
 
+    def take_masters(self):
+        """Masters as the parameters are now (after the parameters were loaded from elsewhere)."""
+        for part in self.parts:
+            part.take_masters()
+
     def moments(self):
         """(m, v) of every tensor as float32 copies, in the parameters' order."""
         out = {}

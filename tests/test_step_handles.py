@@ -298,3 +298,17 @@ def test_a_state_of_parts_goes_to_parts(host):
     for opt, saved in ((mixed, step.state_dict()), (mixed, {"parts": [step.state_dict()]}), (step, mixed.state_dict())):
         with pytest.raises(ValueError):
             opt.load_state_dict(saved)
+
+
+def test_masters_of_every_part_are_taken_anew(host):
+    """A program loads other weights into a model of several types: the masters follow where it says so, the 32-bit part has none."""
+    from paper_2203_09044_amd import MixedAdamW
+    params = [torch.zeros(5), torch.zeros(3, 2).half(), torch.zeros(4).bfloat16(), torch.zeros(2).half()]
+    opt = MixedAdamW(params, [torch.zeros_like(p) for p in params], master=True)
+    for k, p in enumerate(params):
+        p.fill_(k + 1.5)
+    opt.take_masters()
+    by_place = {k: part._views(part.master)[i] for places, part in zip(opt.places, opt.parts) if part.master is not None
+                for i, k in enumerate(places)}
+    assert sorted(by_place) == [1, 2, 3] and all(torch.equal(x, params[k].float()) for k, x in by_place.items())
+    make("mixed")[0].take_masters()                             # without masters there is nothing to take
