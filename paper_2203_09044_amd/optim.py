@@ -290,6 +290,8 @@ class AdamW:
             if lr.dtype != torch.float32 or lr.numel() != 1 or lr.device != self._table.device:
                 raise ValueError("lr: a float32 tensor of one element on the parameters' device")
             if not self._device_steps:              # the device counts from here on
+                if torch.cuda.is_current_stream_capturing():        # and would again at every replay
+                    raise RuntimeError("lr as a tensor inside a capture needs device_steps=True")
                 self._dev[0] = self._t
                 self._device_steps = True
             self._args.lr = 0.0

@@ -312,3 +312,21 @@ def test_masters_of_every_part_are_taken_anew(host):
                 for i, k in enumerate(places)}
     assert sorted(by_place) == [1, 2, 3] and all(torch.equal(x, params[k].float()) for k, x in by_place.items())
     make("mixed")[0].take_masters()                             # without masters there is nothing to take
+
+
+def test_the_device_does_not_begin_to_count_inside_a_capture(host):
+    """The count that the device starts from would be part of the graph, and every replay the same step."""
+    _, _, opt = one_type()
+    opt.step()
+    host.capturing = True
+    with pytest.raises(RuntimeError):
+        opt.lr = torch.tensor([1e-3])
+    host.capturing = False
+    assert opt.lr == 1e-3 and not opt._device_steps and opt._lr_ptr is None
+    opt.step()
+    assert opt.t == 2
+    opt.lr = torch.tensor([1e-3])
+    host.capturing = True
+    opt.lr = torch.tensor([2e-3])                               # the device counts already
+    opt.step()
+    assert int(opt._dev[0]) == 2
