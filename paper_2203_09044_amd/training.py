@@ -102,7 +102,7 @@ class Co3SGD:
         avg = self.pipe.avg if avg is None else avg
         if self.norm is not None:                  # (norm, factor); the factor of a norm that is not finite is -1: no step
             factor = self.norm.compute([avg[:self.n]])[1]
-            avg = torch.where(factor > 0.0, avg[:self.n] * factor, 0.0)
+            avg = torch.where(factor > 0.0, avg[:self.n].float() * factor, 0.0)
         with torch.no_grad():
             for p, a, b in zip(self.params, self.seg_off[:-1], self.seg_off[1:]):
                 p.add_(avg[a:b].view_as(p), alpha=-self.lr)

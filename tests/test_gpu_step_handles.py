@@ -118,3 +118,18 @@ def test_tables_of_different_sizes_take_turns_on_one_workspace(co3):
                 B.step_begin(args, state, work[:at])
                 want = math.sqrt(sum(w * w for _, _, _, w in some))
                 assert near(state.view(torch.float32)[4], want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_sgd_clips_an_average_of_any_type_in_32_bits(co3, dtype):
+    """The average times the factor goes to the weights as a float32 number, whatever the average is kept in: with a small factor
+    a half-precision product would be among the subnormal numbers."""
+    torch.manual_seed(33)
+    model = torch.nn.Linear(48, 30).cuda()
+    opt = co3.Co3SGD(model, 1, co3.Fmt(4, 3), lr=0.5, max_norm=1e-4)
+    avg = torch.randn(opt.n, device="cuda").to(dtype)
+    before = [p.detach().clone() for p in opt.params]
+    opt.apply_average(avg)
+    factor = opt.norm.compute()[1].clone()
+    for p, b, a0, a1 in zip(opt.params, before, opt.seg_off[:-1], opt.seg_off[1:]):
+        assert torch.equal(p.detach(), torch.add(b, (avg[a0:a1].float() * factor).view_as(p), alpha=-0.5))
