@@ -864,3 +864,10 @@ def test_training_with_another_average_and_rate(co3):
         opt.apply_average(avg)
         other.step([avg[a:b] for a, b in zip(opt.seg_off[:-1], opt.seg_off[1:])])
     assert all(torch.equal(a.detach(), b.detach()) for a, b in zip(model.parameters(), ref.parameters()))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("table,skew,gap", [("blocks", 0, 0), ("mixed", 3, 1)])
+@pytest.mark.parametrize("ptype,gtype,master", [(BF16, F32, False), (F16, BF16, False), (BF16, F16, True)])
+def test_steps_of_the_other_types(co3, bits, table, skew, gap, ptype, gtype, master):
+    run_steps(co3, TABLES[table], ptype, gtype, master, bits, skew=skew, gap=gap, max_norm=0.5 if skew else None)
