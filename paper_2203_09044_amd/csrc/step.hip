@@ -5,6 +5,7 @@
 #include "co3_dev.h"
 #include "kernels.h"
 #include "step.h"
+#include "step_root.h"
 
 #define ST_BLOCK 256
 #define ST_NORM_BLOCK (CO3_WAVE * ST_NORM_WAVES)
@@ -344,15 +345,6 @@ __device__ __forceinline__ uint32_t e4m3_scale(uint32_t max_bits)
 {
     const int s = (int)((max_bits + 0x200000u) >> 23) - 8;
     return s > 0 ? (uint32_t)s : 0u;
-}
-// Correctly rounded square root of 0 <= v < 2^40 (compared with the root in 64 bits for every such number): an estimate by
-// the reciprocal root, off by a few units, and one correction by the exactly known rest v - s^2.  The scaling keeps the rest of
-// a small v above the smallest number; the summand gives 0 a finite reciprocal and changes nothing else.  (The
-// compiler's root is right everywhere and takes twice the operations.)
-__device__ __forceinline__ float root_below_2_40(float v)
-{
-    const float x = v * 0x1p80f, y = __builtin_amdgcn_rsqf(x + 0x1p-120f), s = x * y;
-    return __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s) * 0x1p-40f;
 }
 // The largest over the L lanes that share a block, in each of them: rotations within rows of 16 lanes, then across.
 template <int L> __device__ __forceinline__ uint32_t block_max_u32(uint32_t v)
