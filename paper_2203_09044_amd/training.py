@@ -26,6 +26,7 @@ import torch
 from co3_inputs import group_small_tensors, seg_offsets
 
 from . import binding as B
+from ._tensors import look
 from .binding import Fmt
 from .optim import AdamW, GradNorm, MixedAdamW
 from .pipeline import Co3Pipeline
@@ -175,7 +176,7 @@ class Co3AdamW(Co3SGD):
                  weight_decay: float = 0.01, state_bits: int = 32, max_norm: Optional[float] = None, seed: int = 0,
                  decay_vectors: bool = False, **codec):
         super().__init__(model, users, fmt, lr, **codec)
-        self._stepped = self.pipe.avg                     # the average whose segments the optimiser holds
+        self._stepped = look([self.pipe.avg])             # the average whose segments the optimiser holds
         decays = [weight_decay if decay_vectors or p.dim() > 1 else 0.0 for p in self.params]
         types = {p.dtype for p in self.params}
         self.opt = (AdamW if len(types) == 1 else MixedAdamW)(
@@ -190,5 +191,6 @@ class Co3AdamW(Co3SGD):
         step."""
         avg = self.pipe.avg if avg is None else avg
         self.opt.lr = self.lr
-        self.opt.step(None if avg is self._stepped else self._segments(avg))
-        self._stepped = avg
+        seen = look([avg])
+        self.opt.step(None if seen == self._stepped else self._segments(avg))
+        self._stepped = seen

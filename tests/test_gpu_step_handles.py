@@ -133,3 +133,30 @@ def test_sgd_clips_an_average_of_any_type_in_32_bits(co3, dtype):
     factor = opt.norm.compute()[1].clone()
     for p, b, a0, a1 in zip(opt.params, before, opt.seg_off[:-1], opt.seg_off[1:]):
         assert torch.equal(p.detach(), torch.add(b, (avg[a0:a1].float() * factor).view_as(p), alpha=-0.5))
+
+
+def test_an_average_that_lies_elsewhere_now_is_the_one_that_is_stepped(co3):
+    """The same tensor object with other memory, another object of the same memory, and the pipeline's own again."""
+    def run(change):
+        torch.manual_seed(34)
+        model = torch.nn.Linear(48, 30).cuda()
+        opt = co3.Co3AdamW(model, 1, co3.Fmt(4, 3), lr=0.1)
+        avgs = [torch.randn(opt.n, device="cuda") for _ in range(4)]
+        held = avgs[0].clone()
+        opt.apply_average(held)
+        change(opt, held, avgs)
+        opt.pipe.avg[:opt.n] = avgs[3]
+        opt.apply_average()
+        assert opt.opt.t == 4
+        return [p.detach().clone() for p in opt.params]
+
+    def swapped(opt, held, avgs):
+        held.data = avgs[1].clone()
+        opt.apply_average(held)
+        held.copy_(avgs[2])
+        opt.apply_average(held[:])
+
+    def separate(opt, held, avgs):
+        opt.apply_average(avgs[1])
+        opt.apply_average(avgs[2])
+    assert all(torch.equal(a, b) for a, b in zip(run(swapped), run(separate)))
