@@ -3,7 +3,8 @@ pass over all of them.
 
 The handles hold what the calls need on the device (the plan of the tensors' chunks, states, partial sums) and issue
 them; all arithmetic runs in the HIP kernels (``co3_grad_norm``, ``co3_adamw``, ``co3_adamw8``).  Calls are issued on the
-current stream of the tensors' device and return without waiting.
+current stream of the tensors' device and return without waiting.  Calls of one handle, replays of graphs that hold them
+among these, share its workspaces: they must not run at the same time.
 """
 from __future__ import annotations
 
@@ -17,7 +18,12 @@ import numpy as np
 import torch
 
 from . import binding as B
-from ._tensors import look as _look, same as _same
+
+try:
+    from ._tensors import look as _look, same as _same
+except ImportError as e:
+    raise ImportError("the host module _tensors.so is not built, or for another torch; run "
+                      "`python -c 'import __graft_entry__ as g; g.build()'`") from e
 
 PerTensor = Union[float, Sequence[float]]
 
@@ -184,8 +190,8 @@ class GradNorm:
     """Global L2 norm of gradients that lie in many tensors, with the factor that clips it.
 
     ``compute()`` returns a float32 tensor of two on the device, (norm, factor): norm = grad_scale * sqrt(sum g^2),
-    factor = grad_scale * min(1, max_norm / (norm + 1e-6)), or -1 where the norm is not finite.  The tensor is the handle's: the
-    next call overwrites it."""
+    factor = grad_scale * min(1, max_norm / (norm + 1e-6)), or -1 where a gradient is not finite (a norm beyond float32 alone is
+    infinite with its factor right).  The tensor is the handle's: the next call overwrites it."""
 
     def __init__(self, grads: Sequence[torch.Tensor], max_norm: float = math.inf, grad_scale: float = 1.0):
         if not max_norm > 0.0:
@@ -218,8 +224,8 @@ class AdamW:
     state_bits      32: ``m``, ``v`` float32.  8: ``m``, ``r`` float8_e4m3fn with ``m_scale``, ``r_scale`` float8_e8m0fnu per 256 elements
                     (r = sqrt(v)), rounded at random by a hash of ``seed``, the step and the place
     master          16-bit parameters: float32 values kept in ``master``, taken from the parameters at the start
-    max_norm        None, or the global norm beyond which the gradients are scaled down; a step whose norm is not finite changes
-                    nothing and does not count (``skipped``)
+    max_norm        None, or the global norm beyond which the gradients are scaled down; a step with a gradient that is not finite
+                    changes nothing and does not count (``skipped``)
     grad_scale      multiplies every gradient (1 / loss scale, say)
     device_steps    the device counts the steps, which a captured step needs (always so with max_norm or a tensor ``lr``)
 
@@ -403,7 +409,8 @@ class AdamW:
 class MixedAdamW:
     """AdamW over parameters of several types, as of a 16-bit model with 32-bit norms: one part (``AdamW``) per pair of parameter and
     gradient type, all of them one step, clipped by one norm.  Arguments as of ``AdamW``; ``master`` is for the 16-bit parts.
-    ``parts`` hold the states, ``places[k]`` says which of the parameters part k has; the device counts the steps."""
+    ``parts`` hold the states, ``places[k]`` says which of the parameters part k has; the device counts the steps.  8-bit states are
+    rounded by the seed, the step and the place within the part: equal places of two parts take equal random bits."""
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: Union[float, torch.Tensor] = 1e-3,
                  weight_decay: PerTensor = 0.01, lr_scales: PerTensor = 1.0, master: bool = False, max_norm: Optional[float] = None, **kw):
